@@ -15,6 +15,10 @@
  *                      (Section 5.2.2) and Scatter (Section 2.2, Step 2).
  *   spconv_free_map    releases a map's host object.
  *
+ * Next to the layers stand the operators of a transformer over their features (voxels as
+ * tokens, a batch's scenes as documents): spconv_rms_norm, spconv_scaled_linear and
+ * spconv_attention.
+ *
  * Conventions shared by every entry point:
  *   - Pointers named d_* are DEVICE pointers, h_* HOST pointers.  The caller owns
  *     and allocates every buffer, including both workspaces; the library never
@@ -282,6 +286,90 @@ typedef struct {
 } spconv_plan_info;
 int spconv_forward_plan(const spconv_map* m, int c_in, int c_out, int dtype,
                         const spconv_options* opt, spconv_plan_info* info);
+
+/* ------------------------------------------------- transformer operators --
+ * Forward only, asynchronous on `stream`, no host synchronisation.  Row strides (ld_*) are
+ * in elements and at least a row; rows need not follow each other without gaps.  Sums and
+ * statistics are float32. */
+
+/* Root-mean-square norm of the rows of d_x [n][c], with the residual's addition before it:
+ *     s = x + residual;   y = s / sqrt(mean(s^2) + eps) * gamma
+ *   d_residual  NULL (s = x) or [n][c];  d_sum: NULL or [n][c], gets s rounded to `dtype` (may
+ *               be d_x or d_residual; only with a residual).  The norm is that of the unrounded s.
+ *   d_gamma     [c] in `dtype`.
+ *   bits8 == 0: d_y [n][c] in `dtype`; d_scale unused.
+ *   bits8 != 0: d_y [n][c] bytes, e4m3 (OCP: 4 exponent bits, 3 of mantissa, largest 448), and
+ *               d_scale [n][ceil(c / 128)] float32, one for each 128 columns of a row:
+ *               scale = max(max|y| / 448, 2^-126), q = y / scale rounded to nearest even; y is
+ *               q * scale.  c % 16 == 0 (SPCONV_EUNSUPPORTED otherwise).  NaN stays NaN; a block
+ *               with an infinity gets an infinite scale and stands for NaN.
+ * Any c >= 1, any strides; 16-byte accesses where pointers and strides allow them.  d_y must
+ * not overlap the inputs. */
+int spconv_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual,
+                    const void* d_gamma, void* d_sum, int64_t ld_sum, void* d_y, int64_t ld_y, float* d_scale,
+                    int64_t ld_scale, int64_t n, int c, int dtype, int bits8, float eps, void* stream);
+
+/* Product of 8-bit rows and 8-bit weights with scales for blocks of 128:
+ *     y[r][o] = sum_b x_scale[r][b] w_scale[o / 128][b] sum_{i in block b} x[r][i] w[o][i]
+ *   d_x [m][k], d_w [n][k] e4m3 bytes (spconv_rms_norm writes such rows);
+ *   d_x_scale [m][ceil(k / 128)], d_w_scale [ceil(n / 128)][ceil(k / 128)] float32;
+ *   d_y [m][n] in `dtype`; relu != 0 applies max(0, .).
+ * Scaled products and their sums are float32.  In 16-bit types, and more than 64 rows, a block's
+ * 128 products are summed by the 8-bit matrix instruction, which drops a product 2^13 times
+ * smaller than the largest of its group of eight, unless exact != 0: then, as for SPCONV_F32
+ * and few rows always, they are summed in float32, at about half the speed.  k, ld_x and ld_w multiples of 16 (16-byte rows;
+ * SPCONV_EUNSUPPORTED otherwise), d_x and d_w 16-byte aligned; any m and n.  k = 0 gives zeros.
+ * d_y must not overlap the inputs. */
+int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, int64_t ld_x_scale,
+                         const void* d_w, int64_t ld_w, const float* d_w_scale, int64_t ld_w_scale, void* d_y,
+                         int64_t ld_y, int64_t m, int n, int k, int dtype, int relu, int exact,
+                         void* stream);
+
+/* Attention inside the documents (scenes, sequences) of a packed batch.  Document t has the
+ * queries q_start[t] .. q_start[t + 1] and the keys k_start[t] .. k_start[t + 1], or k_len[t]
+ * keys from k_start[t] on (a cache with room to grow; what lies behind them is never read).
+ * Its last query stands at its last key: query i of len_q is at place p = len_k - len_q + i.
+ * It sees key j < len_k if !causal or j < max(p + 1, prefix[t]).  For each head
+ *     s_j = cap tanh(scale q.k_j / cap)   (cap > 0; else scale q.k_j)   - slope dist(i, j)
+ *     out = sum_j softmax(s)_j v_j        over the keys it sees
+ * with dist = |p - j|, or the Euclidean distance of the two voxels where positions are given
+ * (rows (b, x, y, z) as the layers' coordinates; b is not used).  A query that sees no key, or
+ * none with a score above -inf, gets zeros.  Hidden keys' values may be anything, NaN included.
+ * Query head h reads key head h / (heads / kv_heads).
+ *   d_q, d_out  rows n_q, heads, head_dim; d_k, d_v: rows n_k, kv_heads, head_dim, all in `dtype`,
+ *               with strides of rows and heads in elements, multiples of 16 bytes (a slice of
+ *               a fused product will do); head_dim elements follow each other.
+ *   max_q, max_k  at least the longest document's queries and keys: keys behind are not read,
+ *               queries behind get no output.
+ * head_dim a multiple of 8 up to 256, 16-byte aligned pointers.  d_q_start must not descend.
+ * Softmax statistics and sums are float32; the exponentials are rounded to `dtype` for the
+ * product with V. */
+typedef struct {
+  const void* d_q;
+  const void* d_k;
+  const void* d_v;
+  void* d_out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head; /* strides in elements */
+  const int32_t* d_q_start; /* [n_docs + 1] */
+  const int32_t* d_k_start; /* [n_docs + 1] */
+  const int32_t* d_k_len;   /* [n_docs] or NULL */
+  const int32_t* d_prefix;  /* [n_docs] or NULL: no prefix */
+  const float* d_slopes;    /* [heads] or NULL: no bias by distance */
+  const int32_t* d_q_pos;   /* [n_q][4] or NULL, with d_k_pos */
+  const int32_t* d_k_pos;   /* [n_k][4] or NULL */
+  int64_t n_q, n_k;
+  int n_docs, max_q, max_k;
+  int heads, kv_heads, head_dim;
+  int dtype;
+  int causal;
+  float scale, cap; /* cap 0: scores are not capped */
+} spconv_attention_args;
+
+/* Device workspace of spconv_attention: partial results where a launch with few queries splits
+ * its keys; 0 where none are needed (and for invalid arguments).  Goes by sizes only, not by
+ * pointers.  256-byte aligned; calls whose work may overlap need a workspace each. */
+size_t spconv_attention_workspace_bytes(const spconv_attention_args* args);
+int spconv_attention(const spconv_attention_args* args, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------ measurement --
  * Event timing: for every id whose bit is set in `mask`, the library records HIP

@@ -7,6 +7,7 @@ raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -29,7 +30,8 @@ EXPORTED = [
     "spconv_map_n_out", "spconv_map_kvol", "spconv_map_out_coords", "spconv_map_counts",
     "spconv_map_pairs", "spconv_map_copy_pairs", "spconv_map_copy_out_coords", "spconv_free_map",
     "spconv_forward_workspace_bytes", "spconv_forward", "spconv_forward_ex", "spconv_forward_noalloc",
-    "spconv_concat_rows",
+    "spconv_concat_rows", "spconv_rms_norm", "spconv_scaled_linear", "spconv_attention",
+    "spconv_attention_workspace_bytes",
     "spconv_forward_plan", "spconv_profile_enable", "spconv_profile_phase_count",
     "spconv_profile_phase_name", "spconv_profile_read", "spconv_last_error",
 ]
@@ -62,6 +64,18 @@ class PlanInfo(ctypes.Structure):
     _fields_ = [("rows_real", ctypes.c_int64), ("rows_padded", ctypes.c_int64),
                 ("n_gemm_launches", ctypes.c_int), ("t_gather", ctypes.c_int), ("t_scatter", ctypes.c_int),
                 ("grouping", ctypes.c_int), ("gather", ctypes.c_int), ("centre", ctypes.c_int)]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("d_q", "d_k", "d_v", "d_out")]
+                + [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row",
+                                                 "out_head")]
+                + [(n, ctypes.c_void_p) for n in ("d_q_start", "d_k_start", "d_k_len", "d_prefix", "d_slopes", "d_q_pos",
+                                                  "d_k_pos")]
+                + [("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64)]
+                + [(n, ctypes.c_int) for n in ("n_docs", "max_q", "max_k", "heads", "kv_heads", "head_dim", "dtype",
+                                               "causal")]
+                + [("scale", ctypes.c_float), ("cap", ctypes.c_float)])
 
 
 _lib = None
@@ -110,6 +124,16 @@ def lib() -> ctypes.CDLL:
     L.spconv_forward_noalloc.restype = c_int
     L.spconv_concat_rows.argtypes = [vp, c_int, vp, c_int, vp, i64, c_int, vp]
     L.spconv_concat_rows.restype = c_int
+    L.spconv_rms_norm.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, c_int, c_int, c_int,
+                                  ctypes.c_float, vp]
+    L.spconv_rms_norm.restype = c_int
+    L.spconv_scaled_linear.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, c_int, c_int, c_int, c_int, c_int,
+                                       vp]
+    L.spconv_scaled_linear.restype = c_int
+    L.spconv_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttentionArgs)]
+    L.spconv_attention_workspace_bytes.restype = sz
+    L.spconv_attention.argtypes = [ctypes.POINTER(AttentionArgs), vp, sz, vp]
+    L.spconv_attention.restype = c_int
     L.spconv_forward_plan.argtypes = [vp, c_int, c_int, c_int, optp, ctypes.POINTER(PlanInfo)]
     L.spconv_forward_plan.restype = c_int
     L.spconv_profile_enable.argtypes = [ctypes.c_uint64]
@@ -226,6 +250,49 @@ def spconv_concat_rows(a: torch.Tensor, b: torch.Tensor, out: torch.Tensor | Non
                                   _stream(stream))
     _check(st, "spconv_concat_rows")
     return out
+
+
+def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape=None) -> None:
+    """Rows [n][c] with columns that follow each other."""
+    if t.dim() != 2 or t.dtype != dtype or (t.shape[1] > 1 and t.stride(1) != 1) or (
+            shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name}: expected rows {shape or ''} of {dtype}, got {t.dtype} {tuple(t.shape)} with strides "
+                         f"{t.stride()}")
+
+
+def _ld(t: torch.Tensor | None) -> int:
+    """Row stride; that of a single row is its length (torch's may be anything)."""
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def spconv_rms_norm(x: torch.Tensor, residual: torch.Tensor | None, gamma: torch.Tensor, total: torch.Tensor | None,
+                    y: torch.Tensor, scale: torch.Tensor | None, eps: float, stream=None) -> None:
+    n, c = x.shape
+    st = lib().spconv_rms_norm(_ptr(x), _ld(x), _ptr(residual), _ld(residual), _ptr(gamma), _ptr(total), _ld(total),
+                               _ptr(y), _ld(y), _ptr(scale), _ld(scale), n, c, DTYPES[x.dtype],
+                               0 if scale is None else 1, eps, _stream(stream))
+    _check(st, "spconv_rms_norm")
+
+
+def spconv_scaled_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                         y: torch.Tensor, relu: bool = False, exact: bool = False, stream=None) -> None:
+    m, k = x.shape
+    st = lib().spconv_scaled_linear(_ptr(x), _ld(x), _ptr(x_scale), _ld(x_scale), _ptr(w), _ld(w), _ptr(w_scale),
+                                    _ld(w_scale), _ptr(y), _ld(y), m, w.shape[0], k, DTYPES[y.dtype], 1 if relu else 0,
+                                    1 if exact else 0, _stream(stream))
+    _check(st, "spconv_scaled_linear")
+
+
+def spconv_attention_workspace_bytes(args: AttentionArgs) -> int:
+    return int(lib().spconv_attention_workspace_bytes(ctypes.byref(args)))
+
+
+def spconv_attention(args: AttentionArgs, workspace: torch.Tensor | None, stream=None) -> None:
+    st = lib().spconv_attention(ctypes.byref(args), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                _stream(stream))
+    _check(st, "spconv_attention")
 
 
 def spconv_forward_plan(m, c_in: int, c_out: int, dtype: int, opt: Options | None = None) -> PlanInfo:
@@ -386,3 +453,127 @@ def conv(in_coords: torch.Tensor, x: torch.Tensor, w: torch.Tensor, K: int, stri
     km = KernelMap.build(in_coords, K, stride, tensor_stride, mode, out_coords, opt)
     f = Forward(km, x.shape[1], w.shape[2], x.dtype, opt)
     return km, f(x, w)
+
+
+# ----------------------------------------------------------------------------
+# Transformer operators over features (rows are tokens)
+# ----------------------------------------------------------------------------
+
+SCALE_BLOCK = 128  # columns of an 8-bit row (and rows of 8-bit weights) that share a scale
+E4M3 = torch.float8_e4m3fn
+
+
+def rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
+             bits8: bool = False, stream=None):
+    """Root-mean-square norm of the rows of x (+ residual): (y, scale, sum).
+
+    y is in x's type and scale None, or with ``bits8`` y is e4m3 and scale float32 [n][ceil(c / 128)];
+    sum is x + residual in x's type (None without a residual)."""
+    n, c = x.shape
+    _rows("x", x, x.dtype)
+    if x.dtype not in DTYPES:
+        raise ValueError(f"x: {x.dtype} is not one of the layers' types")
+    if gamma.dtype != x.dtype or tuple(gamma.shape) != (c,) or not gamma.is_contiguous():
+        raise ValueError(f"gamma: expected contiguous {x.dtype} {(c,)}, got {gamma.dtype} {tuple(gamma.shape)}")
+    total = scale = None
+    if residual is not None:
+        _rows("residual", residual, x.dtype, (n, c))
+    with _allocate_on(stream):
+        if residual is not None:
+            total = torch.empty((n, c), dtype=x.dtype, device=x.device)
+        y = torch.empty((n, c), dtype=E4M3 if bits8 else x.dtype, device=x.device)
+        if bits8:
+            scale = torch.empty((n, -(-c // SCALE_BLOCK)), dtype=torch.float32, device=x.device)
+    spconv_rms_norm(x, residual, gamma, total, y, scale, eps, stream)
+    return y, scale, total
+
+
+def scaled_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, dtype: torch.dtype,
+                  relu: bool = False, exact: bool = False, stream=None) -> torch.Tensor:
+    """Product of e4m3 rows x [m][k] and e4m3 weights w [n][k] with their scales, in ``dtype``.
+    ``exact``: every sum in float32 also in 16-bit types (slower; spconv_scaled_linear in spconv.h)."""
+    _rows("x", x, E4M3)
+    m, k = x.shape
+    _rows("w", w, E4M3)
+    n, kb = w.shape[0], -(-k // SCALE_BLOCK)
+    if w.shape[1] != k:
+        raise ValueError(f"w: expected [n][{k}], got {tuple(w.shape)}")
+    _rows("x_scale", x_scale, torch.float32, (m, kb))
+    _rows("w_scale", w_scale, torch.float32, (-(-n // SCALE_BLOCK), kb))
+    if dtype not in DTYPES:
+        raise ValueError(f"{dtype} is not one of the layers' types")
+    with _allocate_on(stream):
+        y = torch.empty((m, n), dtype=dtype, device=x.device)
+    spconv_scaled_linear(x, x_scale, w, w_scale, y, relu, exact, stream)
+    return y
+
+
+def quantize_weight(w: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+    """Weights [n][k] as e4m3 and float32 scales of 128 x 128 blocks, for scaled_linear (once,
+    when a model is loaded)."""
+    n, k = w.shape
+    nb, kb = -(-n // SCALE_BLOCK), -(-k // SCALE_BLOCK)
+    full = torch.zeros((nb * SCALE_BLOCK, kb * SCALE_BLOCK), dtype=torch.float32, device=w.device)
+    full[:n, :k] = w
+    blocks = full.view(nb, SCALE_BLOCK, kb, SCALE_BLOCK)
+    scale = (blocks.abs().amax((1, 3)) / 448.0).clamp(min=2.0 ** -126)
+    q = (blocks / scale[:, None, :, None]).view_as(full)[:n, :k].contiguous()
+    return q.clamp(-448.0, 448.0).to(E4M3), scale
+
+
+def _allocate_on(stream):
+    """Memory allocated inside belongs to the stream that the call runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _heads(name: str, t: torch.Tensor, dtype: torch.dtype, head_dim: int) -> None:
+    if t.dim() != 3 or t.dtype != dtype or t.shape[2] != head_dim or t.stride(2) != 1:
+        raise ValueError(f"{name}: expected [rows][heads][{head_dim}] of {dtype}, got {t.dtype} {tuple(t.shape)} with "
+                         f"strides {t.stride()}")
+
+
+def _int32(name: str, t: torch.Tensor | None, shape) -> None:
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected contiguous int32 {shape}, got {t.dtype} {tuple(t.shape)}")
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, k_start: torch.Tensor,
+              max_q: int, max_k: int, k_len: torch.Tensor | None = None, prefix: torch.Tensor | None = None,
+              causal: bool = False, scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
+              q_pos: torch.Tensor | None = None, k_pos: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention inside the documents of a packed batch (spconv_attention in spconv.h).
+
+    q [n_q][heads][d], k and v [n_k][kv_heads][d] may be slices of a fused product; q_start and
+    k_start int32 [docs + 1]; k_len int32 [docs] where k and v are caches; scale defaults to
+    1 / sqrt(d).  Returns [n_q][heads][d]."""
+    n_q, heads, d = q.shape
+    n_k, kv_heads = k.shape[0], k.shape[1]
+    dtype = q.dtype
+    if dtype not in DTYPES:
+        raise ValueError(f"q: {dtype} is not one of the layers' types")
+    _heads("q", q, dtype, d)
+    _heads("k", k, dtype, d)
+    _heads("v", v, dtype, d)
+    if v.shape != k.shape:
+        raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
+    docs = q_start.shape[0] - 1
+    _int32("q_start", q_start, (docs + 1,))
+    _int32("k_start", k_start, (docs + 1,))
+    _int32("k_len", k_len, (docs,))
+    _int32("prefix", prefix, (docs,))
+    _int32("q_pos", q_pos, (n_q, 4))
+    _int32("k_pos", k_pos, (n_k, 4))
+    if slopes is not None and (slopes.dtype != torch.float32 or tuple(slopes.shape) != (heads,)
+                               or not slopes.is_contiguous()):
+        raise ValueError(f"slopes: expected contiguous float32 {(heads,)}, got {slopes.dtype} {tuple(slopes.shape)}")
+    with _allocate_on(stream):
+        out = torch.empty((n_q, heads, d), dtype=dtype, device=q.device)
+    a = AttentionArgs(_ptr(q), _ptr(k), _ptr(v), _ptr(out), q.stride(0), q.stride(1), k.stride(0), k.stride(1),
+                      v.stride(0), v.stride(1), out.stride(0), out.stride(1), _ptr(q_start), _ptr(k_start), _ptr(k_len),
+                      _ptr(prefix), _ptr(slopes), _ptr(q_pos), _ptr(k_pos), n_q, n_k, docs, max_q, max_k, heads, kv_heads,
+                      d, DTYPES[dtype], 1 if causal else 0, d ** -0.5 if scale is None else scale, cap)
+    need = spconv_attention_workspace_bytes(a)
+    with _allocate_on(stream):
+        workspace = _device_bytes(need, q.device) if need else None
+    spconv_attention(a, workspace, stream)
+    return out

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <chrono>
 #include <cstdio>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -10,6 +11,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "attention.h"
 #include "common.h"
 #include "spconv.h"
 
@@ -90,7 +92,8 @@ const char* prof_name(int id) {
       "scatter", "hash", "", "", "", "",
       "k_minmax", "k_radix_hist", "k_radix_scatter", "k_scan", "k_copy", "k_down_keys", "k_unique", "k_backward",
       "k_forward_count", "k_forward_write", "k_fill", "k_radix_local", "k_gather", "k_gemm", "k_scatter", "k_pack",
-      "k_hash_insert", "k_hash_probe", "k_scatter_centre", "k_conv_small", "", "", "", ""};
+      "k_hash_insert", "k_hash_probe", "k_scatter_centre", "k_conv_small", "k_rms_norm", "k_scaled_linear", "k_attention",
+      "k_attention_join"};
   return (id >= 0 && id < PROF_IDS) ? kNames[id] : "";
 }
 struct PhaseRec {
@@ -1087,6 +1090,141 @@ int spconv_forward_noalloc(const spconv_map* m, const void* d_x, const void* d_w
   if ((st = scratch_address(&ws)) != SPCONV_OK) return st;
   return forward_impl(m, d_x, d_w, d_y, c_in, c_out, dtype, d_residual, relu, opt, ws,
                       (size_t)SPCONV_NOALLOC_SCRATCH_BYTES, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Transformer operators
+// ---------------------------------------------------------------------------
+namespace {
+
+bool known_dtype(int dtype) { return dtype == SPCONV_F32 || dtype == SPCONV_F16 || dtype == SPCONV_BF16; }
+bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+int check_attention(const spconv_attention_args* a) {
+  if (!a) return fail(SPCONV_EINVAL, "args is NULL");
+  if (!known_dtype(a->dtype)) return fail(SPCONV_EUNSUPPORTED, "dtype");
+  if (a->n_q < 0 || a->n_k < 0 || a->n_docs < 0 || a->max_q < 0 || a->max_k < 0)
+    return fail(SPCONV_EINVAL, "negative size");
+  if (a->n_q > 0x7fffffff || a->n_k > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads != 0)
+    return fail(SPCONV_EINVAL, "heads must be a multiple of kv_heads");
+  if (a->heads > 65535) return fail(SPCONV_EUNSUPPORTED, "more than 65535 heads");
+  if (a->head_dim < 8 || a->head_dim > 256 || a->head_dim % 8 != 0)
+    return fail(SPCONV_EUNSUPPORTED, "head_dim must be a multiple of 8 up to 256");
+  if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return fail(SPCONV_EINVAL, "scale must be positive and finite");
+  if (!(a->cap >= 0.0f) || !std::isfinite(a->cap)) return fail(SPCONV_EINVAL, "cap must be finite and not negative");
+  if ((a->d_q_pos == nullptr) != (a->d_k_pos == nullptr) || (a->d_q_pos && !a->d_slopes))
+    return fail(SPCONV_EINVAL, "voxels are given for queries and keys, with slopes, or not at all");
+  return SPCONV_OK;
+}
+
+size_t attention_bytes(const spconv_attention_args* a, const AttnPlan& p, void* base, f32x2** ml, float** o) {
+  if (p.splits <= 1) return 0;
+  Bump b(base);
+  const int64_t rows = (int64_t)p.splits * a->n_q * a->heads;
+  f32x2* m = b.take<f32x2>(rows);
+  float* f = b.take<float>(rows * a->head_dim);
+  if (ml) *ml = m;
+  if (o) *o = f;
+  return b.off;
+}
+
+}  // namespace
+
+extern "C" {
+
+int spconv_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, const void* d_gamma,
+                    void* d_sum, int64_t ld_sum, void* d_y, int64_t ld_y, float* d_scale, int64_t ld_scale, int64_t n,
+                    int c, int dtype, int bits8, float eps, void* stream) {
+  if (!known_dtype(dtype)) return fail(SPCONV_EUNSUPPORTED, "dtype");
+  if (n < 0 || c <= 0) return fail(SPCONV_EINVAL, "negative number of rows, or no columns");
+  if (n > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (bits8 && c % 16 != 0) return fail(SPCONV_EUNSUPPORTED, "8-bit rows need 16-byte rows: c % 16 == 0");
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(SPCONV_EINVAL, "eps must be finite and not negative");
+  if (ld_x < c || ld_y < c || (d_residual && ld_residual < c) || (d_sum && ld_sum < c) ||
+      (bits8 && ld_scale < (c + kScaleBlock - 1) / kScaleBlock))
+    return fail(SPCONV_EINVAL, "row stride shorter than a row");
+  if (d_sum && !d_residual) return fail(SPCONV_EINVAL, "d_sum without d_residual");
+  if (n == 0) return SPCONV_OK;
+  if (!d_x || !d_gamma || !d_y || (bits8 && !d_scale)) return fail(SPCONV_EINVAL, "NULL pointer");
+  const uintptr_t e = elem_bytes(dtype);
+  for (const void* p : {d_x, d_residual, d_gamma, (const void*)d_sum, bits8 ? nullptr : (const void*)d_y})
+    if (reinterpret_cast<uintptr_t>(p) % e != 0) return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
+  if (bits8 && reinterpret_cast<uintptr_t>(d_scale) % 4 != 0) return fail(SPCONV_EINVAL, "d_scale must be 4-byte aligned");
+  SPC_TRY(launch_rms_norm(d_x, ld_x, d_residual, ld_residual, d_gamma, d_sum, ld_sum, d_y, ld_y, d_scale, ld_scale, n, c,
+                          dtype, bits8 != 0, eps, static_cast<hipStream_t>(stream)),
+          "norm");
+  return SPCONV_OK;
+}
+
+int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, int64_t ld_x_scale, const void* d_w,
+                         int64_t ld_w, const float* d_w_scale, int64_t ld_w_scale, void* d_y, int64_t ld_y, int64_t m,
+                         int n, int k, int dtype, int relu, int exact, void* stream) {
+  if (!known_dtype(dtype)) return fail(SPCONV_EUNSUPPORTED, "dtype");
+  if (m < 0 || n < 0 || k < 0) return fail(SPCONV_EINVAL, "negative size");
+  if (k % 16 != 0 || (k > 0 && (ld_x % 16 != 0 || ld_w % 16 != 0)))
+    return fail(SPCONV_EUNSUPPORTED, "8-bit rows need 16-byte rows: k, ld_x and ld_w multiples of 16");
+  const int kb = (k + kScaleBlock - 1) / kScaleBlock;
+  if (ld_x < k || ld_w < k || ld_y < n || ld_x_scale < kb || ld_w_scale < kb)
+    return fail(SPCONV_EINVAL, "row stride shorter than a row");
+  if (m > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (m == 0 || n == 0) return SPCONV_OK;
+  if (!d_y || (k > 0 && (!d_x || !d_x_scale || !d_w || !d_w_scale))) return fail(SPCONV_EINVAL, "NULL pointer");
+  if (misaligned16(d_x) || misaligned16(d_w)) return fail(SPCONV_EINVAL, "d_x and d_w must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(d_y) % elem_bytes(dtype) != 0 || reinterpret_cast<uintptr_t>(d_x_scale) % 4 != 0 ||
+      reinterpret_cast<uintptr_t>(d_w_scale) % 4 != 0)
+    return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
+  SPC_TRY(launch_scaled_linear(d_x, ld_x, d_x_scale, ld_x_scale, d_w, ld_w, d_w_scale, ld_w_scale, d_y, ld_y, m, n, k,
+                               dtype, relu, exact != 0, static_cast<hipStream_t>(stream)),
+          "scaled product");
+  return SPCONV_OK;
+}
+
+size_t spconv_attention_workspace_bytes(const spconv_attention_args* a) {
+  if (check_attention(a) != SPCONV_OK) return 0;
+  return attention_bytes(a, attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads), nullptr,
+                         nullptr, nullptr);
+}
+
+int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t ws_bytes, void* stream) {
+  const int st = check_attention(a);
+  if (st != SPCONV_OK) return st;
+  if (a->n_q == 0 || a->n_docs == 0) return SPCONV_OK;
+  if (a->max_q == 0) return fail(SPCONV_EINVAL, "max_q is 0 but there are queries");
+  if (!a->d_q || !a->d_out || !a->d_q_start || !a->d_k_start || (a->n_k > 0 && a->max_k > 0 && (!a->d_k || !a->d_v)))
+    return fail(SPCONV_EINVAL, "NULL pointer");
+  if (misaligned16(a->d_q) || misaligned16(a->d_k) || misaligned16(a->d_v) || misaligned16(a->d_out))
+    return fail(SPCONV_EINVAL, "d_q, d_k, d_v and d_out must be 16-byte aligned");
+  const int64_t e = elem_bytes(a->dtype);
+  for (int64_t stride : {a->q_row, a->q_head, a->k_row, a->k_head, a->v_row, a->v_head, a->out_row, a->out_head})
+    if (stride < 0 || stride * e % 16 != 0) return fail(SPCONV_EUNSUPPORTED, "strides must be multiples of 16 bytes");
+  if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
+    return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
+  const AttnPlan p = attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads);
+  AttnArgs k = {};
+  const size_t need = attention_bytes(a, p, d_workspace, &k.part_ml, &k.part_o);
+  if (need > 0 && (!d_workspace || ws_bytes < need)) return fail(SPCONV_ENOSPC, "attention workspace too small");
+  if (reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0) return fail(SPCONV_EINVAL, "workspace must be 256-byte aligned");
+  constexpr float kLog2e = 1.4426950408889634f;
+  k.q = a->d_q, k.k = a->d_k, k.v = a->d_v, k.out = a->d_out;
+  k.q_row = a->q_row, k.q_head = a->q_head, k.k_row = a->k_row, k.k_head = a->k_head;
+  k.v_row = a->v_row, k.v_head = a->v_head, k.out_row = a->out_row, k.out_head = a->out_head;
+  k.q_start = a->d_q_start, k.k_start = a->d_k_start, k.k_len = a->d_k_len, k.prefix = a->d_prefix;
+  k.slopes = a->d_slopes, k.q_pos = a->d_q_pos, k.k_pos = a->d_k_pos;
+  k.n_q = a->n_q, k.n_k = a->n_k, k.n_docs = a->n_docs, k.max_q = a->max_q, k.max_k = a->max_k;
+  k.heads = a->heads, k.kv_heads = a->kv_heads, k.d = a->head_dim, k.causal = a->causal;
+  k.cap = a->cap;
+  k.cap_log2 = a->cap * kLog2e;
+  k.tanh_by = a->cap > 0.0f ? 2.0f * kLog2e * a->scale / a->cap : 0.0f;
+  k.scale_log2 = a->scale * kLog2e;
+  k.exp_by = a->cap > 0.0f || a->d_slopes ? 1.0f : k.scale_log2;
+  // below every finite score that matters, and finite in both units
+  k.floor = -3e38f / std::max(1.0f, k.exp_by);
+  k.splits = p.splits, k.chunk = p.chunk;
+  SPC_TRY(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention");
+  return SPCONV_OK;
 }
 
 // --------------------------------------------------------------- measurement

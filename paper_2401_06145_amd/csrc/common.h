@@ -107,6 +107,7 @@ enum ProfId : int {
   KN_MINMAX = 16, KN_RADIX_HIST, KN_RADIX_SCATTER, KN_SCAN, KN_COPY, KN_DOWN_KEYS, KN_UNIQUE,
   KN_BACKWARD, KN_FORWARD_COUNT, KN_FORWARD_WRITE, KN_FILL, KN_RADIX_LOCAL, KN_GATHER, KN_GEMM, KN_SCATTER,
   KN_PACK, KN_HASH_INSERT, KN_HASH_PROBE, KN_SCATTER_CENTRE, KN_CONV_SMALL,
+  KN_RMS_NORM, KN_SCALED_LINEAR, KN_ATTENTION, KN_ATTENTION_JOIN,
   PROF_IDS = 40
 };
 struct ProfScope {
@@ -301,5 +302,16 @@ hipError_t launch_conv_small(const void* x, int64_t n_in, const void* w, const i
                              int64_t mt_stride, const uint32_t* perm, int64_t pairs, int K3, void* y,
                              const void* residual, int relu, int64_t n_out, int c_in, int c_out, int dtype,
                              hipStream_t s);
+
+// norm.hip: rows' root-mean-square norm with the residual's addition; y in the rows' type,
+// or e4m3 with a scale per 128 columns (bits8).  sum, residual: NULL or rows like x.
+hipError_t launch_rms_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* gamma, void* sum,
+                           int64_t ld_sum, void* y, int64_t ld_y, float* scales, int64_t ld_scales, int64_t n, int c,
+                           int dtype, bool bits8, float eps, hipStream_t s);
+// linear8.hip: e4m3 rows times e4m3 weights [n][k], scaled by blocks of 128.
+hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, int64_t ld_xs, const void* w, int64_t ld_w,
+                                const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
+                                int relu, bool exact, hipStream_t s);
+// (attention.hip: attention.h)
 
 }  // namespace spc

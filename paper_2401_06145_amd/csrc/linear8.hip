@@ -1,0 +1,286 @@
+// Product of 8-bit rows and 8-bit weights (e4m3), with a float32 scale for each row and 128
+// columns of the rows and for each 128 x 128 block of the weights:
+//   y[r][n] = relu?( sum_b xs[r][b] ws[n / 128][b] sum_{k in block b} x[r][k] w[n][k] )
+//
+// One matrix instruction multiplies 16 weights' rows by 16 rows over exactly one block of
+// 128 columns (v_mfma_f32_16x16x128_f8f6f4); its float32 result is scaled and added to the
+// float32 sums with one fma an element.
+#include <algorithm>
+#include <type_traits>
+
+#include "rows.h"
+
+namespace spc {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct LinearArgs {
+  const uint8_t* x;
+  const float* xs;
+  const uint8_t* w;
+  const float* ws;
+  void* y;
+  int64_t ld_x, ld_xs, ld_w, ld_ws, ld_y;
+  int64_t m;
+  int n, k, kb;  // kb: blocks of 128 columns
+  int relu;
+  int wide_y;  // rows of y take 16-byte stores
+};
+
+// Eight e4m3 numbers as float16, exactly.
+__device__ __forceinline__ f16x8 widen(uint32_t lo, uint32_t hi) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Product over a block of 128 columns: 32 consecutive bytes of a row a lane.  The 8-bit
+// instruction drops a product that is 2^13 times smaller than the largest of its group of
+// eight (measured): at most 7 2^-13 of the sum of magnitudes, and 1.4e-5 of the result where
+// rows are quantised from normal values, which a 16-bit result's rounding covers.  EXACT
+// widens both operands to float16, which holds every e4m3 number, and sums their products in
+// float32, at half the rate.
+template <bool EXACT>
+__device__ __forceinline__ f32x4 mma128(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1) {
+  if constexpr (!EXACT) {
+    const i32x8 a = __builtin_bit_cast(i32x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+    const i32x8 b = __builtin_bit_cast(i32x8, __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7));
+    // both operands e4m3, hardware scales 2^0 (127 in each byte)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0,
+                                                            0x7f7f7f7f);
+  } else {
+    f32x4 t = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 &x = i < 2 ? a0 : a1, &y = i < 2 ? b0 : b1;
+      t = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(x[i % 2 * 2], x[i % 2 * 2 + 1]),
+                                                 widen(y[i % 2 * 2], y[i % 2 * 2 + 1]), t, 0, 0, 0);
+    }
+    return t;
+  }
+}
+
+// `count` consecutive outputs (a multiple of 4) of one row from column n0 on.
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_y(const LinearArgs& a, int64_t row, int n0, const float* v) {
+  if (row >= a.m) return;
+  T* y = static_cast<T*>(a.y) + row * a.ld_y + n0;
+  float r[COUNT];
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) r[i] = a.relu ? (v[i] < 0.0f ? 0.0f : v[i]) : v[i];
+  constexpr int V = 16 / (int)sizeof(T) < COUNT ? 16 / (int)sizeof(T) : COUNT;
+#pragma unroll
+  for (int i = 0; i < COUNT; i += V) {
+    if (a.wide_y && n0 + i + V <= a.n) {
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4*>(y + i) = f32x4{r[i], r[i + 1], r[i + 2], r[i + 3]};
+      } else if constexpr (V == 8) {
+        *reinterpret_cast<u32x4*>(y + i) = u32x4{pack2<T>(r[i], r[i + 1]), pack2<T>(r[i + 2], r[i + 3]),
+                                                 pack2<T>(r[i + 4], r[i + 5]), pack2<T>(r[i + 6], r[i + 7])};
+      } else {
+        *reinterpret_cast<u32x2*>(y + i) = u32x2{pack2<T>(r[i], r[i + 1]), pack2<T>(r[i + 2], r[i + 3])};
+      }
+    } else {
+#pragma unroll
+      for (int j = i; j < i + V; ++j)
+        if (n0 + j < a.n) y[j] = (T)r[j];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles: a workgroup of WM x WN waves takes BM rows and BN outputs, a block of 128
+// columns at a time through LDS.  Rows of 128 bytes; the 16-byte chunk c of row r lies at
+// chunk c ^ (r / 2 % 8), so that 16 lanes reading one chunk of 16 rows meet every bank once.
+// ---------------------------------------------------------------------------
+template <typename T, bool EXACT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs a) {
+  constexpr int TH = 64 * WM * WN;
+  constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
+  constexpr int PX = BM * 8 / TH, PW = BN * 8 / TH;  // 16-byte chunks a thread stages
+  __shared__ __align__(16) u32x4 sx[BM * 8], sw[BN * 8];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int wm = wave / WN, wn = wave % WN;
+  const int r16 = lane % 16, g = lane / 16;
+  const int64_t m0 = (int64_t)blockIdx.y * BM;
+  const int n0 = blockIdx.x * BN;
+
+  const uint8_t* px[PX];
+  const uint8_t* pw[PW];
+  int sat_x[PX], sat_w[PW];
+#pragma unroll
+  for (int i = 0; i < PX; ++i) {
+    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8;
+    px[i] = a.x + std::min<int64_t>(m0 + r, a.m - 1) * a.ld_x + 16 * c;
+    sat_x[i] = r * 8 + (c ^ (r / 2 % 8));
+  }
+  // LDS row 16 t + 4 q + b of a wave's weights holds output 4 NT q + 4 t + b, so that a lane
+  // ends with 4 NT consecutive outputs of its row
+#pragma unroll
+  for (int i = 0; i < PW; ++i) {
+    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8;
+    const int in = r % (16 * NT), out = r - in + 4 * NT * (in / 4 % 4) + 4 * (in / 16) + in % 4;
+    pw[i] = a.w + (int64_t)std::min(n0 + out, a.n - 1) * a.ld_w + 16 * c;
+    sat_w[i] = r * 8 + (c ^ (r / 2 % 8));
+  }
+  const float* xs[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+    xs[i] = a.xs + std::min<int64_t>(m0 + wm * 16 * MT + 16 * i + r16, a.m - 1) * a.ld_xs;
+  const float* ws = a.ws + (int64_t)std::min((n0 + wn * 16 * NT) / kScaleBlock, (a.n - 1) / kScaleBlock) * a.ld_ws;
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+  for (int b = 0; b < a.kb; ++b) {
+    const int left = a.k - b * kScaleBlock;  // columns of this block that exist
+    u32x4 vx[PX], vw[PW];
+#pragma unroll
+    for (int i = 0; i < PX; ++i) {
+      vx[i] = u32x4{0, 0, 0, 0};
+      if (16 * (int)((threadIdx.x + TH * i) % 8) < left)
+        vx[i] = *reinterpret_cast<const u32x4*>(px[i] + (int64_t)b * kScaleBlock);
+    }
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      vw[i] = u32x4{0, 0, 0, 0};
+      if (16 * (int)((threadIdx.x + TH * i) % 8) < left)
+        vw[i] = *reinterpret_cast<const u32x4*>(pw[i] + (int64_t)b * kScaleBlock);
+    }
+    const float sb = ws[b];
+    float scale[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) scale[i] = xs[i][b] * sb;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PX; ++i) sx[sat_x[i]] = vx[i];
+#pragma unroll
+    for (int i = 0; i < PW; ++i) sw[sat_w[i]] = vw[i];
+    __syncthreads();
+    u32x4 fw[NT][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int r = wn * 16 * NT + 16 * j + r16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fw[j][h] = sw[r * 8 + ((2 * g + h) ^ (r / 2 % 8))];
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int r = wm * 16 * MT + 16 * i + r16;
+      const u32x4 f0 = sx[r * 8 + ((2 * g) ^ (r / 2 % 8))], f1 = sx[r * 8 + ((2 * g + 1) ^ (r / 2 % 8))];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const f32x4 t = mma128<EXACT>(fw[j][0], fw[j][1], f0, f1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(scale[i], t[e], acc[i][j][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    float v[4 * NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
+    store_y<T, 4 * NT>(a, m0 + wm * 16 * MT + 16 * i + r16, n0 + wn * 16 * NT + 4 * NT * g, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a workgroup takes 16 outputs and all rows (16 MT of them); its waves share the
+// blocks of 128 columns out among themselves and add their sums through LDS at the end.
+// Weights go from memory straight into registers: a matrix operand's lane reads 32
+// consecutive bytes of its row, four lanes a whole 128-byte line.
+// ---------------------------------------------------------------------------
+template <typename T, int MT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_linear_rows(LinearArgs a) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int r16 = lane % 16, g = lane / 16;
+  const int n0 = blockIdx.x * 16;
+  const uint8_t* w = a.w + (int64_t)std::min(n0 + r16, a.n - 1) * a.ld_w + 32 * g;
+  const float* ws = a.ws + (int64_t)(n0 / kScaleBlock) * a.ld_ws;
+  const uint8_t* x[MT];
+  const float* xs[MT];
+  f32x4 acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = std::min<int64_t>(16 * i + r16, a.m - 1);
+    x[i] = a.x + row * a.ld_x + 32 * g;
+    xs[i] = a.xs + row * a.ld_xs;
+    acc[i] = f32x4{0, 0, 0, 0};
+  }
+  const u32x4 zero = {0, 0, 0, 0};
+  for (int b = wave; b < a.kb; b += WAVES) {
+    const int at = b * kScaleBlock;
+    const bool h0 = at + 32 * g < a.k, h1 = at + 32 * g + 16 < a.k;
+    const u32x4 w0 = h0 ? *reinterpret_cast<const u32x4*>(w + at) : zero;
+    const u32x4 w1 = h1 ? *reinterpret_cast<const u32x4*>(w + at + 16) : zero;
+    const float sb = ws[b];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const u32x4 x0 = h0 ? *reinterpret_cast<const u32x4*>(x[i] + at) : zero;
+      const u32x4 x1 = h1 ? *reinterpret_cast<const u32x4*>(x[i] + at + 16) : zero;
+      const float scale = xs[i][b] * sb;
+      const f32x4 t = mma128<true>(w0, w1, x0, x1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(scale, t[e], acc[i][e]);
+    }
+  }
+  __shared__ f32x4 part[WAVES][MT][kWave];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  for (int i = wave; i < MT; i += WAVES) {
+    f32x4 v = part[0][i][lane];
+#pragma unroll
+    for (int q = 1; q < WAVES; ++q) v += part[q][i][lane];
+    float r[4] = {v[0], v[1], v[2], v[3]};
+    store_y<T, 4>(a, 16 * i + r16, n0 + 4 * g, r);
+  }
+}
+
+template <typename T>
+void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
+  if (a.m <= 64) {
+    const dim3 grid((unsigned)((a.n + 15) / 16));
+#define SPC_R(MT) hipLaunchKernelGGL((k_linear_rows<T, MT, 8>), grid, dim3(512), 0, s, a)
+    if (a.m <= 16) SPC_R(1);
+    else if (a.m <= 32) SPC_R(2);
+    else SPC_R(4);
+#undef SPC_R
+    return;
+  }
+  const dim3 grid((unsigned)((a.n + 127) / 128), (unsigned)((a.m + 127) / 128));
+  if constexpr (!std::is_same_v<T, float>) {
+    if (!exact) {
+      hipLaunchKernelGGL((k_linear_tile<T, false, 128, 128, 2, 2>), grid, dim3(256), 0, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_linear_tile<T, true, 128, 128, 2, 2>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, int64_t ld_xs, const void* w, int64_t ld_w,
+                                const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
+                                int relu, bool exact, hipStream_t s) {
+  if (m <= 0 || n <= 0) return hipSuccess;
+  if ((m + 127) / 128 > 65535) return hipErrorInvalidValue;
+  ProfScope ps(KN_SCALED_LINEAR, s);
+  const int64_t e = dtype == 0 ? 4 : 2;
+  LinearArgs a = {static_cast<const uint8_t*>(x), xs, static_cast<const uint8_t*>(w), ws, y, ld_x, ld_xs, ld_w, ld_ws,
+                  ld_y, m, n, k, (k + kScaleBlock - 1) / kScaleBlock, relu, 0};
+  a.wide_y = reinterpret_cast<uintptr_t>(y) % 16 == 0 && ld_y * e % 16 == 0;
+  if (dtype == 0) linear_t<float>(a, true, s);
+  else if (dtype == 1) linear_t<_Float16>(a, exact, s);
+  else linear_t<__bf16>(a, exact, s);
+  return hipGetLastError();
+}
+
+}  // namespace spc

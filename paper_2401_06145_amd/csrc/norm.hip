@@ -1,0 +1,213 @@
+// Root-mean-square norm of rows with the residual's addition before it, the result in the
+// rows' type or in 8 bits with a scale for each 128 columns:
+//   s = x + residual,  y = s / sqrt(mean(s^2) + eps) * gamma
+//   8 bits: scale = max(max|y| / 448, 2^-126) of each 128 columns, q = e4m3(y / scale)
+//
+// A row is read once and stays in registers, in float32, between the sum of squares and
+// the output; the norm is that of the unrounded sum.  What bounds it is memory: 16-bit
+// rows with a residual move 7 bytes an element (x, residual, sum, q).
+#include <algorithm>
+#include <type_traits>
+
+#include "rows.h"
+
+namespace spc {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct NormArgs {
+  const void* x;
+  const void* res;
+  const void* gamma;
+  void* sum;
+  void* y;
+  float* scales;
+  int64_t ld_x, ld_res, ld_sum, ld_y, ld_scales;
+  int64_t n;
+  int c;
+  float eps;
+};
+
+// G lanes per row (a power of two up to a workgroup), CH chunks of 8 columns per lane.
+// Chunk i of a lane is columns 8 (i G + lane): 16 neighbouring lanes hold one scale block.
+template <typename T, bool Q8, int G, int CH>
+__global__ __launch_bounds__(kThreads) void k_rms_norm(NormArgs a) {
+  const int lane = threadIdx.x % G;
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  const bool mine = row < a.n;  // a wave's other rows may still be there: no return before the shuffles
+  const T* x = static_cast<const T*>(a.x) + (mine ? row : 0) * a.ld_x;
+  const T* res = a.res ? static_cast<const T*>(a.res) + (mine ? row : 0) * a.ld_res : nullptr;
+  float v[CH][8];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int col = 8 * (i * G + lane);
+    if (mine && col < a.c) {
+      load8(x + col, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+    }
+  }
+  if (res) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int col = 8 * (i * G + lane);
+      if (mine && col < a.c) {
+        float r[8];
+        load8(res + col, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += r[j];
+        if (a.sum) store8(static_cast<T*>(a.sum) + row * a.ld_sum + col, v[i]);
+      }
+    }
+  }
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq = fmaf(v[i][j], v[i][j], sq);
+#pragma unroll
+  for (int m = 1; m < (G < kWave ? G : kWave); m *= 2) sq += __shfl_xor(sq, m);
+  if constexpr (G > kWave) {
+    __shared__ float part[kThreads / kWave];
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sq;
+    __syncthreads();
+    sq = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) sq += part[w];
+  }
+  const float inv = 1.0f / sqrtf(sq / (float)a.c + a.eps);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int col = 8 * (i * G + lane);
+    const bool in = mine && col < a.c;
+    float w[8];
+    if (in) {
+      load8(static_cast<const T*>(a.gamma) + col, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = v[i][j] * inv * w[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = 0.0f;
+    }
+    if constexpr (Q8) {
+      float top = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(w[j]));
+#pragma unroll
+      for (int m = 1; m < kScaleBlock / 8; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+      const float scale = block_scale(top), by = 1.0f / scale;
+      if (in) {
+        const u32x2 q = {pack_e4m3(w[0] * by, w[1] * by, w[2] * by, w[3] * by),
+                         pack_e4m3(w[4] * by, w[5] * by, w[6] * by, w[7] * by)};
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.y) + row * a.ld_y + col) = q;
+        if (lane % (kScaleBlock / 8) == 0) a.scales[row * a.ld_scales + col / kScaleBlock] = scale;
+      }
+    } else if (in) {
+      store8(static_cast<T*>(a.y) + row * a.ld_y + col, w);
+    }
+  }
+}
+
+// Any width, stride and alignment: a workgroup per row, element by element; the row is
+// read again (from cache) for its output.
+template <typename T, bool Q8>
+__global__ __launch_bounds__(kThreads) void k_rms_norm_any(NormArgs a) {
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+  const T* res = a.res ? static_cast<const T*>(a.res) + row * a.ld_res : nullptr;
+  const T* gamma = static_cast<const T*>(a.gamma);
+  const auto at = [&](int col) { return (float)x[col] + (res ? (float)res[col] : 0.0f); };
+  float sq = 0.0f;
+  for (int col = threadIdx.x; col < a.c; col += kThreads) {
+    const float s = at(col);
+    sq = fmaf(s, s, sq);
+  }
+#pragma unroll
+  for (int m = 1; m < kWave; m *= 2) sq += __shfl_xor(sq, m);
+  __shared__ float part[kThreads / kWave];
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sq;
+  __syncthreads();
+  sq = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) sq += part[w];
+  const float inv = 1.0f / sqrtf(sq / (float)a.c + a.eps);
+  // a wave takes a scale block at a time, two columns a lane.  The sum may be stored over
+  // x or the residual: each element is read before it is written, by the same lane
+  for (int b = threadIdx.x / kWave; b * kScaleBlock < a.c; b += kThreads / kWave) {
+    const int col = b * kScaleBlock + 2 * (threadIdx.x % kWave);
+    float w[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (col + j < a.c) {
+        const float s = at(col + j);
+        if (res && a.sum) static_cast<T*>(a.sum)[row * a.ld_sum + col + j] = (T)s;
+        w[j] = s * inv * (float)gamma[col + j];
+      }
+    }
+    if constexpr (Q8) {
+      float top = fmaxf(fabsf(w[0]), fabsf(w[1]));
+#pragma unroll
+      for (int m = 1; m < kWave; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+      const float scale = block_scale(top), by = 1.0f / scale;
+      const uint32_t q = pack_e4m3(w[0] * by, w[1] * by, 0.0f, 0.0f);
+      uint8_t* y = static_cast<uint8_t*>(a.y) + row * a.ld_y;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (col + j < a.c) y[col + j] = (uint8_t)(q >> (8 * j));
+      if (threadIdx.x % kWave == 0) a.scales[row * a.ld_scales + b] = scale;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (col + j < a.c) static_cast<T*>(a.y)[row * a.ld_y + col + j] = (T)w[j];
+    }
+  }
+}
+
+template <typename T, bool Q8>
+void norm_t(const NormArgs& a, bool wide, hipStream_t s) {
+  const int chunks = (a.c + 7) / 8;
+  if (!wide || chunks > kThreads * 8) {
+    hipLaunchKernelGGL((k_rms_norm_any<T, Q8>), dim3((unsigned)a.n), dim3(kThreads), 0, s, a);
+    return;
+  }
+#define SPC_N(G, CH)                                                                                             \
+  hipLaunchKernelGGL((k_rms_norm<T, Q8, G, CH>), dim3((unsigned)((a.n + kThreads / G - 1) / (kThreads / G))), \
+                     dim3(kThreads), 0, s, a)
+  if (chunks <= 16) SPC_N(16, 1);
+  else if (chunks <= 32) SPC_N(32, 1);
+  else if (chunks <= 64) SPC_N(64, 1);
+  else if (chunks <= 128) SPC_N(64, 2);
+  else if (chunks <= 256) SPC_N(64, 4);
+  else if (chunks <= 512) SPC_N(64, 8);
+  else if (chunks <= 1024) SPC_N(256, 4);
+  else SPC_N(256, 8);
+#undef SPC_N
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* gamma, void* sum,
+                           int64_t ld_sum, void* y, int64_t ld_y, float* scales, int64_t ld_scales, int64_t n, int c,
+                           int dtype, bool bits8, float eps, hipStream_t s) {
+  if (n <= 0) return hipSuccess;
+  if (n > 0x7fffffff) return hipErrorInvalidValue;
+  ProfScope ps(KN_RMS_NORM, s);
+  const int64_t e = dtype == 0 ? 4 : 2;
+  const auto fits = [](const void* p, int64_t ld, int64_t elem, int64_t by) {
+    return !p || (reinterpret_cast<uintptr_t>(p) % by == 0 && ld * elem % by == 0);
+  };
+  // whole 16-byte accesses, where every row of every array allows them
+  const bool wide = c % 8 == 0 && fits(x, ld_x, e, 16) && fits(res, ld_res, e, 16) && fits(gamma, 0, e, 16) &&
+                    fits(sum, ld_sum, e, 16) && (bits8 ? fits(y, ld_y, 1, 8) : fits(y, ld_y, e, 16));
+  const NormArgs a = {x, res, gamma, sum, y, scales, ld_x, ld_res, ld_sum, ld_y, ld_scales, n, c, eps};
+#define SPC_N(T) (bits8 ? norm_t<T, true>(a, wide, s) : norm_t<T, false>(a, wide, s))
+  if (dtype == 0) SPC_N(float);
+  else if (dtype == 1) SPC_N(_Float16);
+  else SPC_N(__bf16);
+#undef SPC_N
+  return hipGetLastError();
+}
+
+}  // namespace spc

@@ -1,0 +1,280 @@
+"""spconv_attention against the formula in 64 bits: documents, caches, masks, caps, biases,
+head layouts, widths, values that no query may see."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2401_06145_amd import binding as B
+from tests import transformer_ref as ref
+from tests.gpu_helpers import DEV, say
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def starts(lens):
+    return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device=DEV)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+class Batch:
+    """Queries, keys and values of documents; room > 0: caches of that many rows, the rest of which
+    holds NaN."""
+
+    def __init__(self, q_lens, k_lens, heads, kv_heads, d, dtype, room=0, seed=1, spread=1.0):
+        g = torch.Generator(DEV).manual_seed(seed)
+        self.q_lens, self.k_lens = q_lens, k_lens
+        self.q = (spread * torch.randn((sum(q_lens), heads, d), device=DEV, generator=g)).to(dtype)
+        self.k_starts = None
+        if room:
+            n = room * len(k_lens)
+            self.k = torch.full((n, kv_heads, d), float("nan"), device=DEV, dtype=dtype)
+            self.v = torch.full_like(self.k, float("nan"))
+            self.k_starts = [room * t for t in range(len(k_lens))]
+            for a, n in zip(self.k_starts, k_lens):
+                self.k[a:a + n] = torch.randn((n, kv_heads, d), device=DEV, generator=g).to(dtype)
+                self.v[a:a + n] = torch.randn((n, kv_heads, d), device=DEV, generator=g).to(dtype)
+            self.args = dict(k_start=ints(self.k_starts + [room * len(k_lens)]), k_len=ints(k_lens))
+        else:
+            n = sum(k_lens)
+            self.k, self.v = (torch.randn((n, kv_heads, d), device=DEV, generator=g).to(dtype) for _ in range(2))
+            self.args = dict(k_start=starts(k_lens))
+        self.slopes = torch.exp2(-1.0 - torch.arange(heads, device=DEV) % 7)
+        self.q_pos, self.k_pos = (torch.randint(-300, 300, (len(t), 4), device=DEV, generator=g, dtype=torch.int32)
+                                  for t in (self.q, self.k))
+
+    def run(self, prefix=None, bias="none", **kw):
+        return B.attention(self.q, self.k, self.v, starts(self.q_lens), max_q=max(self.q_lens), max_k=max(self.k_lens),
+                           prefix=None if prefix is None else ints(prefix), **self.args, **self.bias(bias), **kw)
+
+    def bias(self, bias):
+        return {"none": {}, "position": dict(slopes=self.slopes),
+                "voxel": dict(slopes=self.slopes / 8, q_pos=self.q_pos, k_pos=self.k_pos)}[bias]
+
+    def check(self, what="", **kw):
+        bias = self.bias(kw.pop("bias", "none"))
+        got = self.run(bias="none", **kw, **bias)
+        want, mag = ref.attention(self.q, self.k, self.v, self.q_lens, self.k_lens, self.k_starts, **kw, **bias)
+        ref.check_attention(got, want, mag, what)
+        return got
+
+
+# queries of each document, its keys (None: the same), heads, key heads, width
+LAYOUTS = [
+    ([1], [1], 1, 1, 8), ([1], [2049], 8, 2, 64), ([1, 1, 1, 1, 1], [5, 0, 700, 31, 32], 4, 4, 32),
+    ([1] * 7, [1, 64, 65, 127, 128, 129, 1000], 32, 8, 128), ([1, 1], [333, 4], 6, 2, 80), ([1], [100], 3, 1, 256),
+    ([2, 1, 5, 3], [2, 100, 77, 3], 8, 4, 96), ([16, 9], [400, 9], 4, 1, 64), ([17], [517], 5, 1, 16),
+    ([130, 0, 1, 63], None, 4, 2, 64), ([300], None, 2, 2, 32), ([65, 200], [65, 1000], 4, 2, 128),
+    ([77], [6000], 3, 3, 40), ([128, 129, 127], None, 8, 8, 32), ([257], None, 2, 1, 256), ([500, 33], None, 6, 2, 80),
+    ([40, 150], [10, 60], 2, 2, 64),  # more queries than keys: the first ones see nothing if causal
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+def test_attention(layout, dtype):
+    ql, kl, heads, kv, d = LAYOUTS[layout]
+    kl = kl or ql
+    say(f"attention {ql} queries, {kl} keys, {heads}/{kv} heads of {d}, {dtype}")
+    b = Batch(ql, kl, heads, kv, d, dtype, seed=layout)
+    b.check("all keys")
+    b.check("causal", causal=True)
+    b.check("causal, prefix", causal=True, prefix=[n // 2 + t for t, n in enumerate(kl)])
+    b.check("capped", cap=3.0)
+    b.check("bias by position", causal=True, bias="position")
+    b.check("bias by distance of voxels", bias="voxel")
+    b.check("all of it", causal=True, prefix=[n // 3 for n in kl], cap=20.0, bias="voxel", scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("queries", [1, 3, 70])
+def test_attention_over_caches(queries, dtype):
+    """Rows of a cache behind a document's keys hold NaN and are never part of a result."""
+    say(f"attention over caches, {queries} queries, {dtype}")
+    kl = [0, 3, 250, 700, 64, 513]
+    b = Batch([min(queries, max(1, n)) for n in kl], kl, 8, 2, 64, dtype, room=800)
+    got = b.check("cache", causal=True)
+    assert bool((got[0] == 0).all())
+    b.check("cache, bias", causal=True, bias="position", cap=10.0)
+
+
+def test_long_cache_is_split_and_joined():
+    say("attention over a long cache")
+    b = Batch([1, 1], [20_001, 17], 4, 1, 128, BF16)
+    b.slopes = b.slopes / 2000
+    B.spconv_profile_read(reset=True)
+    B.spconv_profile_enable(True)
+    try:
+        b.check("long", causal=True)
+        b.check("long, bias", causal=True, bias="position")
+        torch.cuda.synchronize()
+    finally:
+        B.spconv_profile_enable(False)
+    got = B.spconv_profile_read(reset=True)
+    assert got["k_attention"][1] == 2 and got["k_attention_join"][1] == 2
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("spread", [6.0, 30.0])
+def test_sharp_scores(spread, dtype):
+    """Scores far apart: the running maximum grows late, most exponentials vanish."""
+    say(f"attention with sharp scores {spread} {dtype}")
+    b = Batch([150, 1], [900, 2000], 4, 2, 64, dtype, spread=spread)
+    got = b.run(causal=True)
+    want, mag = ref.attention(b.q, b.k, b.v, b.q_lens, b.k_lens, causal=True)
+    # scores of size 8 spread carry float32 errors of their own
+    u = ref.UNIT[dtype]
+    bound = mag * (2 * u + 4e-5 * spread) + want.abs() * u + ref.TINY[dtype]
+    assert bool(((got.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("kind", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("lens", [([200], [200]), ([3, 2], [100, 50]), ([70], [333])])
+def test_hidden_values_do_not_matter(lens, kind, dtype):
+    """What stands in keys and values that a query does not see has no part in its result, in its
+    own tile neither; queries that see it do get it."""
+    say(f"attention with {kind} in hidden rows, {lens}, {dtype}")
+    ql, kl = lens
+    b = Batch(ql, kl, 4, 2, 64, dtype)
+    clean = b.run(causal=True)
+    at = kl[0] - 2  # seen by the last two queries of the first document
+    for part in ("k", "v"):
+        d = Batch(ql, kl, 4, 2, 64, dtype)
+        getattr(d, part)[at, 0, 5] = float(kind)
+        got = d.run(causal=True)
+        sees = torch.zeros(len(b.q), dtype=torch.bool, device=DEV)
+        sees[ql[0] - 2:ql[0]] = True
+        assert torch.equal(got[~sees], clean[~sees]), part
+        assert torch.equal(got[:, 2:], clean[:, 2:]), part  # the other key head
+        mine = got[sees][:, :2]
+        if part == "v":
+            assert not bool(mine[..., 5].isfinite().any())
+            assert torch.equal(mine[..., 6:], clean[sees][:, :2, 6:])
+            if kind != "nan":
+                assert bool((mine[..., 5] == float(kind)).all())
+        elif kind == "nan":
+            assert bool(mine.isnan().all())
+
+
+def test_a_row_of_minus_infinities_gives_zeros():
+    say("attention where every score is -inf")
+    b = Batch([1, 40], [30, 40], 2, 2, 32, F32)
+    b.q[0, 0] = 1.0
+    b.k[:30, 0] = -float("inf")
+    got = b.run()
+    assert bool((got[0, 0] == 0).all()) and bool(got[0, 1].isfinite().all()) and bool((got[0, 1] != 0).any())
+
+
+@pytest.mark.parametrize("d,heads,kv", [(64, 4, 2), (80, 6, 3), (32, 8, 8)])
+def test_slices_of_a_fused_product(d, heads, kv):
+    say(f"attention on slices, {heads}/{kv} heads of {d}")
+    n = 333
+    g = torch.Generator(DEV).manual_seed(3)
+    rows = torch.randn((n, (heads + 2 * kv) * d + 16), device=DEV, generator=g).to(BF16)
+    q, k, v = (t.unflatten(1, (-1, d)) for t in rows[:, 16:].split([heads * d, kv * d, kv * d], 1))
+    lens = [200, 133]
+    s = starts(lens)
+    for most in (200,):
+        got = B.attention(q, k, v, s, s, most, most, causal=True)
+        want, mag = ref.attention(q, k, v, lens, lens, causal=True)
+        ref.check_attention(got, want, mag, "slices")
+    # heads before rows
+    qt, kt, vt = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v))
+    assert torch.equal(B.attention(qt, kt, vt, s, s, 200, 200, causal=True), got)
+
+
+def test_a_key_of_a_huge_cache():
+    """Offsets of more than 2^31 elements, and of more than 2^32 bytes."""
+    say("attention at the end of a cache of 2^31 elements")
+    rows, kv, d = (1 << 31) // (8 * 128) + 600, 8, 128
+    k, v = (torch.empty((rows, kv, d), dtype=F16, device=DEV) for _ in range(2))
+    g = torch.Generator(DEV).manual_seed(4)
+    n = 500
+    k[-n:], v[-n:] = (torch.randn((n, kv, d), device=DEV, generator=g).to(F16) for _ in range(2))
+    for ql in (1, 100):
+        q = torch.randn((ql, 16, d), device=DEV, generator=g).to(F16)
+        got = B.attention(q, k, v, ints([0, ql]), ints([rows - n, rows]), ql, n, causal=True)
+        want, mag = ref.attention(q, k[-n:].contiguous(), v[-n:].contiguous(), [ql], [n], causal=True)
+        ref.check_attention(got, want, mag, f"{ql} queries")
+
+
+def test_lengths_beyond_the_stated_ones_are_not_read():
+    say("attention, max_k shorter than a document")
+    b = Batch([1], [600], 2, 1, 64, F16)
+    got = B.attention(b.q, b.k, b.v, ints([0, 1]), ints([0, 600]), 1, 256)
+    want, mag = ref.attention(b.q, b.k[:256], b.v[:256], [1], [256])
+    ref.check_attention(got, want, mag, "first 256 keys")
+
+
+@pytest.mark.parametrize("docs", [1, 63, 64, 65, 200, 4500])
+def test_many_documents(docs):
+    say(f"attention over {docs} documents")
+    for most in (6, 40):
+        ql = [(t * 7 + 3) % (most + 1) for t in range(docs)]
+        if max(ql) < most:
+            ql[0] = most
+        b = Batch(ql, ql, 4, 2, 16, F16, seed=docs)
+        got = b.run(causal=True)
+        few = sorted({0, 1, docs // 2, docs - 2, docs - 1} & set(range(docs)))
+        at = [sum(ql[:t]) for t in range(docs + 1)]
+        for t in few:
+            rows = slice(at[t], at[t + 1])
+            want, mag = ref.attention(b.q[rows], b.k[rows], b.v[rows], [ql[t]], [ql[t]], causal=True)
+            ref.check_attention(got[rows], want, mag, f"document {t}")
+        assert bool(got.isfinite().all())
+
+
+def test_attention_repeats_to_the_bit():
+    say("attention, repeated")
+    for b in (Batch([1] * 9, [3000] * 9, 8, 2, 128, BF16), Batch([700, 50], [700, 900], 4, 2, 64, F16)):
+        a = b.run(causal=True)
+        assert all(torch.equal(b.run(causal=True), a) for _ in range(3))
+
+
+def test_attention_on_another_stream():
+    say("attention on another stream")
+    b = Batch([1, 1], [5000, 300], 8, 1, 64, F16)
+    want = b.run(causal=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = b.run(causal=True, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
+
+
+def test_operators_in_a_graph():
+    """Captured once, replayed with other inputs in the same places and eager work between."""
+    say("operators captured in a graph")
+    c, heads, d, n = 256, 4, 64, 90
+    g = torch.Generator(DEV).manual_seed(5)
+    x = torch.randn((n, c), device=DEV, generator=g).to(BF16)
+    gamma = torch.ones(c, device=DEV, dtype=BF16)
+    w, ws = B.quantize_weight(torch.randn((3 * c, c), device=DEV, generator=g) / c ** 0.5)
+    lens = [1, 89]
+    s = starts(lens)
+    cache = torch.randn((2, 4000, heads, d), device=DEV, generator=g).to(BF16)
+    long, one = ints([0, 4000]), ints([0, 1])
+
+    def step():
+        q8, scale, _ = B.rms_norm(x, gamma, bits8=True)
+        q, k, v = (t.unflatten(1, (heads, d)) for t in B.scaled_linear(q8, scale, w, ws, BF16).split(c, 1))
+        return B.attention(q, k, v, s, s, 89, 89, causal=True), B.attention(q[:1], cache[0], cache[1], one, long, 1, 4000)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for turn in range(4):
+        x.copy_(torch.randn((n, c), device=DEV, generator=g).to(BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {turn}"
