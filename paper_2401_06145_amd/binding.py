@@ -7,7 +7,6 @@ raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -252,37 +251,44 @@ def spconv_concat_rows(a: torch.Tensor, b: torch.Tensor, out: torch.Tensor | Non
     return out
 
 
-def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape=None) -> None:
+def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, n: int, c: int) -> None:
     """Rows [n][c] with columns that follow each other."""
-    if t.dim() != 2 or t.dtype != dtype or (t.shape[1] > 1 and t.stride(1) != 1) or (
-            shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name}: expected rows {shape or ''} of {dtype}, got {t.dtype} {tuple(t.shape)} with strides "
+    if t.dtype is not dtype or t.shape != (n, c) or (c > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected rows {(n, c)} of {dtype}, got {t.dtype} {tuple(t.shape)} with strides "
                          f"{t.stride()}")
 
 
-def _ld(t: torch.Tensor | None) -> int:
+def _ld(t: torch.Tensor) -> int:
     """Row stride; that of a single row is its length (torch's may be anything)."""
-    if t is None:
-        return 0
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    n, c = t.shape
+    return t.stride(0) if n > 1 else max(t.stride(0), c)
+
+
+def _device_stream(t: torch.Tensor, stream=None) -> int:
+    """The stream's handle; by default the current one of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def spconv_rms_norm(x: torch.Tensor, residual: torch.Tensor | None, gamma: torch.Tensor, total: torch.Tensor | None,
                     y: torch.Tensor, scale: torch.Tensor | None, eps: float, stream=None) -> None:
     n, c = x.shape
-    st = lib().spconv_rms_norm(_ptr(x), _ld(x), _ptr(residual), _ld(residual), _ptr(gamma), _ptr(total), _ld(total),
-                               _ptr(y), _ld(y), _ptr(scale), _ld(scale), n, c, DTYPES[x.dtype],
-                               0 if scale is None else 1, eps, _stream(stream))
-    _check(st, "spconv_rms_norm")
+    res, ld_res = (None, 0) if residual is None else (residual.data_ptr(), _ld(residual))
+    out, ld_out = (None, 0) if total is None else (total.data_ptr(), _ld(total))
+    bits8, sc, ld_sc = (0, None, 0) if scale is None else (1, scale.data_ptr(), _ld(scale))
+    st = lib().spconv_rms_norm(x.data_ptr(), _ld(x), res, ld_res, gamma.data_ptr(), out, ld_out, y.data_ptr(), _ld(y), sc,
+                               ld_sc, n, c, DTYPES[x.dtype], bits8, eps, _device_stream(x, stream))
+    if st:
+        _check(st, "spconv_rms_norm")
 
 
 def spconv_scaled_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                          y: torch.Tensor, relu: bool = False, exact: bool = False, stream=None) -> None:
     m, k = x.shape
-    st = lib().spconv_scaled_linear(_ptr(x), _ld(x), _ptr(x_scale), _ld(x_scale), _ptr(w), _ld(w), _ptr(w_scale),
-                                    _ld(w_scale), _ptr(y), _ld(y), m, w.shape[0], k, DTYPES[y.dtype], 1 if relu else 0,
-                                    1 if exact else 0, _stream(stream))
-    _check(st, "spconv_scaled_linear")
+    st = lib().spconv_scaled_linear(x.data_ptr(), _ld(x), x_scale.data_ptr(), _ld(x_scale), w.data_ptr(), _ld(w),
+                                    w_scale.data_ptr(), _ld(w_scale), y.data_ptr(), _ld(y), m, w.shape[0], k,
+                                    DTYPES[y.dtype], relu, exact, _device_stream(x, stream))
+    if st:
+        _check(st, "spconv_scaled_linear")
 
 
 def spconv_attention_workspace_bytes(args: AttentionArgs) -> int:
@@ -290,9 +296,14 @@ def spconv_attention_workspace_bytes(args: AttentionArgs) -> int:
 
 
 def spconv_attention(args: AttentionArgs, workspace: torch.Tensor | None, stream=None) -> None:
-    st = lib().spconv_attention(ctypes.byref(args), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                _stream(stream))
-    _check(st, "spconv_attention")
+    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    st = lib().spconv_attention(ctypes.byref(args), ws, n, stream)
+    if st:
+        _check(st, "spconv_attention")
 
 
 def spconv_forward_plan(m, c_in: int, c_out: int, dtype: int, opt: Options | None = None) -> PlanInfo:
@@ -463,6 +474,14 @@ SCALE_BLOCK = 128  # columns of an 8-bit row (and rows of 8-bit weights) that sh
 E4M3 = torch.float8_e4m3fn
 
 
+def _empty(shape, dtype, like: torch.Tensor, stream=None) -> torch.Tensor:
+    """Device memory that belongs to the stream which the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
              bits8: bool = False, stream=None):
     """Root-mean-square norm of the rows of x (+ residual): (y, scale, sum).
@@ -470,20 +489,19 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: torch.Tensor | None
     y is in x's type and scale None, or with ``bits8`` y is e4m3 and scale float32 [n][ceil(c / 128)];
     sum is x + residual in x's type (None without a residual)."""
     n, c = x.shape
-    _rows("x", x, x.dtype)
-    if x.dtype not in DTYPES:
-        raise ValueError(f"x: {x.dtype} is not one of the layers' types")
-    if gamma.dtype != x.dtype or tuple(gamma.shape) != (c,) or not gamma.is_contiguous():
-        raise ValueError(f"gamma: expected contiguous {x.dtype} {(c,)}, got {gamma.dtype} {tuple(gamma.shape)}")
+    dtype = x.dtype
+    if dtype not in DTYPES:
+        raise ValueError(f"x: {dtype} is not one of the layers' types")
+    _rows("x", x, dtype, n, c)
+    if gamma.dtype is not dtype or gamma.shape != (c,) or not gamma.is_contiguous():
+        raise ValueError(f"gamma: expected contiguous {dtype} {(c,)}, got {gamma.dtype} {tuple(gamma.shape)}")
     total = scale = None
     if residual is not None:
-        _rows("residual", residual, x.dtype, (n, c))
-    with _allocate_on(stream):
-        if residual is not None:
-            total = torch.empty((n, c), dtype=x.dtype, device=x.device)
-        y = torch.empty((n, c), dtype=E4M3 if bits8 else x.dtype, device=x.device)
-        if bits8:
-            scale = torch.empty((n, -(-c // SCALE_BLOCK)), dtype=torch.float32, device=x.device)
+        _rows("residual", residual, dtype, n, c)
+        total = _empty((n, c), dtype, x, stream)
+    y = _empty((n, c), E4M3 if bits8 else dtype, x, stream)
+    if bits8:
+        scale = _empty((n, -(-c // SCALE_BLOCK)), torch.float32, x, stream)
     spconv_rms_norm(x, residual, gamma, total, y, scale, eps, stream)
     return y, scale, total
 
@@ -492,18 +510,15 @@ def scaled_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_sca
                   relu: bool = False, exact: bool = False, stream=None) -> torch.Tensor:
     """Product of e4m3 rows x [m][k] and e4m3 weights w [n][k] with their scales, in ``dtype``.
     ``exact``: every sum in float32 also in 16-bit types (slower; spconv_scaled_linear in spconv.h)."""
-    _rows("x", x, E4M3)
     m, k = x.shape
-    _rows("w", w, E4M3)
     n, kb = w.shape[0], -(-k // SCALE_BLOCK)
-    if w.shape[1] != k:
-        raise ValueError(f"w: expected [n][{k}], got {tuple(w.shape)}")
-    _rows("x_scale", x_scale, torch.float32, (m, kb))
-    _rows("w_scale", w_scale, torch.float32, (-(-n // SCALE_BLOCK), kb))
+    _rows("x", x, E4M3, m, k)
+    _rows("w", w, E4M3, n, k)
+    _rows("x_scale", x_scale, torch.float32, m, kb)
+    _rows("w_scale", w_scale, torch.float32, -(-n // SCALE_BLOCK), kb)
     if dtype not in DTYPES:
         raise ValueError(f"{dtype} is not one of the layers' types")
-    with _allocate_on(stream):
-        y = torch.empty((m, n), dtype=dtype, device=x.device)
+    y = _empty((m, n), dtype, x, stream)
     spconv_scaled_linear(x, x_scale, w, w_scale, y, relu, exact, stream)
     return y
 
@@ -521,20 +536,17 @@ def quantize_weight(w: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
     return q.clamp(-448.0, 448.0).to(E4M3), scale
 
 
-def _allocate_on(stream):
-    """Memory allocated inside belongs to the stream that the call runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
-
-
 def _heads(name: str, t: torch.Tensor, dtype: torch.dtype, head_dim: int) -> None:
-    if t.dim() != 3 or t.dtype != dtype or t.shape[2] != head_dim or t.stride(2) != 1:
+    if t.dim() != 3 or t.dtype is not dtype or t.shape[2] != head_dim or t.stride(2) != 1:
         raise ValueError(f"{name}: expected [rows][heads][{head_dim}] of {dtype}, got {t.dtype} {tuple(t.shape)} with "
                          f"strides {t.stride()}")
 
 
-def _int32(name: str, t: torch.Tensor | None, shape) -> None:
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+def _int32(name: str, t: torch.Tensor, shape) -> int:
+    """The address of a contiguous int32 array."""
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous int32 {shape}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, k_start: torch.Tensor,
@@ -557,23 +569,19 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.
     if v.shape != k.shape:
         raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
     docs = q_start.shape[0] - 1
-    _int32("q_start", q_start, (docs + 1,))
-    _int32("k_start", k_start, (docs + 1,))
-    _int32("k_len", k_len, (docs,))
-    _int32("prefix", prefix, (docs,))
-    _int32("q_pos", q_pos, (n_q, 4))
-    _int32("k_pos", k_pos, (n_k, 4))
-    if slopes is not None and (slopes.dtype != torch.float32 or tuple(slopes.shape) != (heads,)
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.shape != (heads,)
                                or not slopes.is_contiguous()):
         raise ValueError(f"slopes: expected contiguous float32 {(heads,)}, got {slopes.dtype} {tuple(slopes.shape)}")
-    with _allocate_on(stream):
-        out = torch.empty((n_q, heads, d), dtype=dtype, device=q.device)
-    a = AttentionArgs(_ptr(q), _ptr(k), _ptr(v), _ptr(out), q.stride(0), q.stride(1), k.stride(0), k.stride(1),
-                      v.stride(0), v.stride(1), out.stride(0), out.stride(1), _ptr(q_start), _ptr(k_start), _ptr(k_len),
-                      _ptr(prefix), _ptr(slopes), _ptr(q_pos), _ptr(k_pos), n_q, n_k, docs, max_q, max_k, heads, kv_heads,
-                      d, DTYPES[dtype], 1 if causal else 0, d ** -0.5 if scale is None else scale, cap)
+    out = _empty((n_q, heads, d), dtype, q, stream)
+    a = AttentionArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *q.stride()[:2], *k.stride()[:2],
+                      *v.stride()[:2], heads * d, d, _int32("q_start", q_start, (docs + 1,)),
+                      _int32("k_start", k_start, (docs + 1,)), None if k_len is None else _int32("k_len", k_len, (docs,)),
+                      None if prefix is None else _int32("prefix", prefix, (docs,)),
+                      None if slopes is None else slopes.data_ptr(),
+                      None if q_pos is None else _int32("q_pos", q_pos, (n_q, 4)),
+                      None if k_pos is None else _int32("k_pos", k_pos, (n_k, 4)), n_q, n_k, docs, max_q, max_k, heads,
+                      kv_heads, d, DTYPES[dtype], causal, d ** -0.5 if scale is None else scale, cap)
     need = spconv_attention_workspace_bytes(a)
-    with _allocate_on(stream):
-        workspace = _device_bytes(need, q.device) if need else None
-    spconv_attention(a, workspace, stream)
+    workspace = _empty(need, torch.uint8, q, stream) if need else None
+    spconv_attention(a, workspace, _device_stream(q, stream))
     return out

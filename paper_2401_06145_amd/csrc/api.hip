@@ -1200,6 +1200,8 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   const int64_t e = elem_bytes(a->dtype);
   for (int64_t stride : {a->q_row, a->q_head, a->k_row, a->k_head, a->v_row, a->v_head, a->out_row, a->out_head})
     if (stride < 0 || stride * e % 16 != 0) return fail(SPCONV_EUNSUPPORTED, "strides must be multiples of 16 bytes");
+  if (a->k_row * e > kMostRowBytes || a->v_row * e > kMostRowBytes)
+    return fail(SPCONV_EUNSUPPORTED, "rows of d_k and d_v at most 32 MiB apart");
   if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
     return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
   const AttnPlan p = attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads);
@@ -1218,11 +1220,11 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   k.cap = a->cap;
   k.cap_log2 = a->cap * kLog2e;
   k.tanh_by = a->cap > 0.0f ? 2.0f * kLog2e * a->scale / a->cap : 0.0f;
-  k.scale_log2 = a->scale * kLog2e;
-  k.exp_by = a->cap > 0.0f || a->d_slopes ? 1.0f : k.scale_log2;
+  k.slope_by = a->cap > 0.0f ? kLog2e : 1.0f / a->scale;
+  k.exp_by = a->cap > 0.0f ? 1.0f : a->scale * kLog2e;
   // below every finite score that matters, and finite in both units
   k.floor = -3e38f / std::max(1.0f, k.exp_by);
-  k.splits = p.splits, k.chunk = p.chunk;
+  k.slots = (int)p.slots, k.splits = p.splits, k.chunk = p.chunk;
   SPC_TRY(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention");
   return SPCONV_OK;
 }

@@ -6,6 +6,8 @@
 namespace spc {
 
 constexpr int kQueryTile = 128;  // queries of a workgroup of the many-query form
+// Strides of key and value rows, in bytes: a tile's rows are addressed with 32 bits.
+constexpr int64_t kMostRowBytes = 1 << 25;
 
 struct AttnArgs {
   const void* q;
@@ -25,9 +27,10 @@ struct AttnArgs {
   float cap;         // > 0: scores are capped
   float cap_log2;    // cap log2(e)
   float tanh_by;     // 2 log2(e) scale / cap
-  float scale_log2;  // scale log2(e)
-  float exp_by;      // from the running maximum's units to log2
+  float slope_by;    // from the slopes' units to the scores'
+  float exp_by;      // from the scores' units to log2
   float floor;       // where the running maximum starts
+  int slots;          // of query tiles (many-query form)
   int splits, chunk;  // key ranges, and keys of each
   f32x2* part_ml;     // [splits][n_q][heads] maximum and sum of a range
   float* part_o;      // [splits][n_q][heads][d] its unnormalised output
@@ -43,5 +46,8 @@ struct AttnPlan {
 };
 AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+// attention_tile.hip, attention_rows.hip: the two forms.
+hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attention_rows(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 
 }  // namespace spc

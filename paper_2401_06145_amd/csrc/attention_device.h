@@ -1,0 +1,233 @@
+// Device code that both forms of the attention share.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attention.h"
+#include "rows.h"
+
+namespace spc {
+namespace attn {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Matrix products on 8 consecutive elements a lane.  mma32: 32 x 32 over 16; lane l holds row
+// (column) l % 32 and elements 8 (l / 32) + j.  mma16: 16 x 16 over 32, row l % 16, elements
+// 8 (l / 16) + j.  float32 goes as eight products, the j-th over every lane's element j.
+template <typename T>
+struct Mat;
+template <>
+struct Mat<_Float16> {
+  typedef f16x8 Frag;
+  __device__ static f32x16 mma32(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  __device__ static f32x4 mma16(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mat<__bf16> {
+  typedef bf16x8 Frag;
+  __device__ static f32x16 mma32(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  __device__ static f32x4 mma16(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mat<float> {
+  typedef f32x8 Frag;
+  __device__ static f32x16 mma32(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+  __device__ static f32x4 mma16(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// A fragment from 8 consecutive elements in memory (16-byte aligned).
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag load_frag(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  } else {
+    return *reinterpret_cast<const typename Mat<T>::Frag*>(p);
+  }
+}
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag zero_frag() {
+  typename Mat<T>::Frag f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = (T)0.0f;
+  return f;
+}
+// Eight float32 values as a fragment, rounded to nearest even.
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag to_frag(const float* v) {
+  if constexpr (sizeof(T) == 4) {
+    return f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  } else {
+    return __builtin_bit_cast(typename Mat<T>::Frag, (u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]),
+                                                            pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])}));
+  }
+}
+
+// Whether any of the elements in 16 bytes is an infinity or not a number.
+template <typename T>
+__device__ __forceinline__ bool odd_values(u32x4 w) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      bad |= (w[i] & 0x7f800000u) == 0x7f800000u;
+    } else {
+      constexpr uint32_t e = std::is_same_v<T, __bf16> ? 0x7f80u : 0x7c00u;
+      bad |= (w[i] & e) == e || (w[i] & (e << 16)) == (e << 16);
+    }
+  }
+  return bad;
+}
+// 1 where an element is NaN (kind 0), +inf (1) or -inf (2); and the value that it adds.
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag odd_ones(typename Mat<T>::Frag f, int kind) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = (float)f[j];
+    const bool is = kind == 0 ? v != v : v == (kind == 1 ? INFINITY : -INFINITY);
+    f[j] = (T)(is ? 1.0f : 0.0f);
+  }
+  return f;
+}
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag finite_only(typename Mat<T>::Frag f) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = (float)f[j];
+    f[j] = fabsf(v) < INFINITY ? f[j] : (T)0.0f;
+  }
+  return f;
+}
+__device__ __forceinline__ int odd_kind(float v) { return v != v ? 0 : v == INFINITY ? 1 : v == -INFINITY ? 2 : -1; }
+__device__ __forceinline__ float odd_value(int kind) { return kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY; }
+
+// Rows of a K or V tile in LDS, in 16-byte chunks that are exchanged inside a row so that the
+// lanes of one access meet different banks: K is read as one chunk of 16 (32) rows, V as 64
+// (32) bytes of 4 (16) rows.
+template <int ROW_BYTES>
+struct Lds {
+  static constexpr uint32_t CH = ROW_BYTES / 16;                         // chunks of a row
+  static constexpr uint32_t R = ROW_BYTES >= 256 ? 1 : 256 / ROW_BYTES;  // rows in 256 bytes
+  __device__ static uint32_t k_chunk(uint32_t row, uint32_t c) { return c ^ (row / R & (CH < 16 ? CH - 1 : 15)); }
+  __device__ static uint32_t v_chunk(uint32_t row, uint32_t c) { return c ^ ((row / R & (CH < 16 ? CH / 4 - 1 : 3)) << 2); }
+  __device__ static uint32_t v_chunk16(uint32_t row, uint32_t c) { return c ^ ((row / R & (CH < 16 ? CH / 2 - 1 : 7)) << 1); }
+};
+
+// Four consecutive rows' elements of one column for every lane of a group of 16: lane i gives
+// the address of four columns of row i / 4, and gets column i of the four rows.
+__device__ __forceinline__ i16x4 read_columns(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) i16x4*)(__attribute__((address_space(3))) const void*)p);
+}
+
+// A document's part of the batch.
+struct Doc {
+  int q0, len_q;
+  int64_t k0;
+  int len_k, prefix;
+};
+__device__ __forceinline__ Doc load_doc(const AttnArgs& a, int doc) {
+  Doc d;
+  d.q0 = std::max(a.q_start[doc], 0);
+  d.len_q = std::min((int)std::min<int64_t>(a.q_start[doc + 1], a.n_q) - d.q0, a.max_q);
+  d.k0 = std::max(a.k_start[doc], 0);
+  const int64_t len = a.k_len ? a.k_len[doc] : a.k_start[doc + 1] - d.k0;
+  d.len_k = (int)std::max<int64_t>(0, std::min<int64_t>(std::min<int64_t>(len, a.max_k), a.n_k - d.k0));
+  d.prefix = a.prefix ? a.prefix[doc] : 0;
+  return d;
+}
+// Number of keys that query i sees: the first ones of its document.
+__device__ __forceinline__ int seen(const AttnArgs& a, const Doc& d, int i) {
+  if (!a.causal) return d.len_k;
+  return std::min(std::max(std::max(d.len_k - d.len_q + i + 1, d.prefix), 0), d.len_k);
+}
+
+// The largest document whose first slot is at most `slot`; slots of document t start at
+// q_start[t] / tile + t, so each has room for its tiles and no running sum is needed.
+__device__ __forceinline__ int find_doc(const AttnArgs& a, int slot, int tile, int* first) {
+  const int lane = threadIdx.x % kWave;
+  int lo = 0, n = a.n_docs;
+  while (true) {
+    const int step = (n + kWave - 1) / kWave, at = lane * step;
+    const bool ok = at < n && a.q_start[lo + at] / tile + lo + at <= slot;
+    const int c = std::max(popc64(__ballot(ok)) - 1, 0);
+    lo += c * step;
+    n = std::min(step, n - c * step);
+    if (step == 1) break;
+  }
+  *first = a.q_start[lo] / tile + lo;
+  return lo;
+}
+
+// Turns products q.k of one query into the scores that the running maximum is taken of;
+// key(i) is the document's key of product i.  Capped scores are in units of log2; the others
+// stay in those of the bare products (exp_by folds their scale into the exponential's).
+// Hidden keys get -inf.
+struct Query {
+  float place, slope;  // place among the keys; slope in the scores' units
+  float x, y, z;       // voxel
+  int lim;             // keys seen
+};
+template <int COUNT, typename Key, typename Pos>
+__device__ __forceinline__ void to_scores(const AttnArgs& a, const Query& q, float* s, bool masked, Key key, Pos pos) {
+  if (a.cap > 0.0f) {
+    // tanh(u) = 1 - 2 / (1 + e^{2u}): exact limits at both ends, absolute error 2^-23
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const float e = __builtin_amdgcn_exp2f(s[i] * a.tanh_by);
+      s[i] = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + e), a.cap_log2);
+    }
+  }
+  if (a.slopes) {
+    if (a.k_pos) {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) {
+        const f32x4 p = pos(i);
+        const float dx = p[0] - q.x, dy = p[1] - q.y, dz = p[2] - q.z;
+        s[i] = fmaf(-q.slope, __builtin_amdgcn_sqrtf(fmaf(dx, dx, fmaf(dy, dy, dz * dz))), s[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) s[i] = fmaf(-q.slope, fabsf(q.place - (float)key(i)), s[i]);
+    }
+  }
+  if (masked) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i] = key(i) < q.lim ? s[i] : -INFINITY;
+  }
+}
+
+__device__ __forceinline__ Query make_query(const AttnArgs& a, const Doc& d, int i, int head) {
+  Query q;
+  q.lim = seen(a, d, i);
+  q.place = (float)(d.len_k - d.len_q + i);
+  q.slope = a.slopes ? a.slopes[head] * a.slope_by : 0.0f;
+  q.x = q.y = q.z = 0.0f;
+  if (a.q_pos) {
+    const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + i);
+    q.x = (float)p[1], q.y = (float)p[2], q.z = (float)p[3];
+  }
+  return q;
+}
+
+// Four consecutive values of a row of the output, or of its partial result.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* v) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  else *reinterpret_cast<u32x2*>(p) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+}
+
+}  // namespace attn
+}  // namespace spc

@@ -1,0 +1,267 @@
+// Attention with few queries per document (one new token over a cache, above all).
+#include "attention_device.h"
+
+namespace spc {
+namespace {
+using namespace attn;
+
+// ---------------------------------------------------------------------------
+// Few queries: a workgroup takes the queries of all heads that share one key head (up to 16
+// NC of them as columns) and one range of keys; its four waves go through the range 32 keys
+// at a time, each on its own, and join their results through LDS at the end.  K comes from
+// memory straight into registers, V through a strip of LDS that only its wave uses.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int NC>
+__global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
+  typedef typename Mat<T>::Frag Frag;
+  constexpr int E = sizeof(T), ROW = D * E, KT = 32;
+  typedef Lds<ROW> L;
+  constexpr int P = KT * L::CH / kWave;
+  constexpr int STRIP = KT * ROW > D * 16 * 4 ? KT * ROW : D * 16 * 4;
+  __shared__ __align__(16) char strips[4][STRIP];
+  __shared__ f32x4 spos[4][KT];
+  __shared__ float sm[4][16 * NC], sl[4][16 * NC];
+
+  const int doc = blockIdx.z, kvh = blockIdx.y;
+  const Doc d = load_doc(a, doc);
+  const int group = a.heads / a.kv_heads, cols = d.len_q * group;
+  if (cols <= 0) return;
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, c16 = lane % 16, g = lane / 16;
+  char* sv = strips[wave];
+
+  Query q[NC];
+  Frag fq[NC][D / 32];
+  int64_t row[NC];  // row of the packed queries times heads, plus the head
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int col = std::min(16 * n + c16, cols - 1), i = col / group, head = kvh * group + col % group;
+    row[n] = (int64_t)(d.q0 + i) * a.heads + head;
+    q[n] = make_query(a, d, i, head);
+    const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + i) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+      const int at = 32 * k + 8 * g;
+      fq[n][k] = at < a.d ? load_frag(p + at) : zero_frag<T>();
+    }
+  }
+  const int lim_lo = seen(a, d, 0), lim_hi = seen(a, d, d.len_q - 1);
+  const int k_begin = blockIdx.x * a.chunk, k_end = std::min(lim_hi, k_begin + a.chunk);
+
+  f32x4 o[NC][D / 16];
+  float m[NC], l[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    m[n] = a.floor;
+    l[n] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[n][t] = f32x4{0, 0, 0, 0};
+  }
+  const T* kp = static_cast<const T*>(a.k) + d.k0 * a.k_row + (int64_t)kvh * a.k_head;
+  const T* vp = static_cast<const T*>(a.v) + d.k0 * a.v_row + (int64_t)kvh * a.v_head;
+
+  for (int k0 = k_begin + wave * KT; k0 < k_end; k0 += 4 * KT) {
+    const bool masked = k0 + KT > lim_lo;
+    Frag fk[2][D / 32];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int key = k0 + 16 * h + c16;
+      const T* p = kp + (int64_t)key * a.k_row;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        const int at = 32 * k + 8 * g;
+        fk[h][k] = key < d.len_k && at < a.d ? load_frag(p + at) : zero_frag<T>();
+      }
+    }
+    bool bad = false;
+    u32x4 rv[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lane + kWave * i, r = p / L::CH, c = p % L::CH;
+      rv[i] = u32x4{0, 0, 0, 0};
+      if (k0 + r < d.len_k && c * (16 / E) < a.d)
+        rv[i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
+      if (masked) bad |= odd_values<T>(rv[i]);
+    }
+    if (a.k_pos && lane < KT) {
+      f32x4 pos = {0, 0, 0, 0};
+      if (k0 + lane < d.len_k) {
+        const int32_t* p = a.k_pos + 4 * (d.k0 + k0 + lane);
+        pos = f32x4{(float)p[1], (float)p[2], (float)p[3], 0};
+      }
+      spos[wave][lane] = pos;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lane + kWave * i, r = p / L::CH, c = p % L::CH;
+      *reinterpret_cast<u32x4*>(sv + r * ROW + 16 * L::v_chunk16(r, c)) = rv[i];
+    }
+    const bool careful = masked && __any(bad);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    Frag fp[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) s[h] = Mat<T>::mma16(fk[h][k], fq[n][k], s[h]);
+      float sc[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sc[i] = s[i / 4][i % 4];
+      const auto at = [&](int i) { return 16 * (i / 4) + 4 * g + i % 4; };
+      to_scores<8>(a, q[n], sc, masked, [&](int i) { return k0 + at(i); }, [&](int i) { return spos[wave][at(i)]; });
+      float top = m[n];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, sc[i]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m[n])) {
+        const float by = __builtin_amdgcn_exp2f((m[n] - top) * a.exp_by);
+        l[n] *= by;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][t][i] *= by;
+        m[n] = top;
+      }
+      const float off = m[n] * a.exp_by;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.exp_by, -off));
+        l[n] += sc[i];
+      }
+      fp[n] = to_frag<T>(sc);
+    }
+    // columns of V: rows 16 t .. of out^T and keys {4 g + j, 16 + 4 g + j}
+    const auto columns = [&](int t) {
+      Frag f;
+      if constexpr (E == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int r = 16 * (j / 4) + 4 * g + j % 4, x = 16 * t + c16;
+          f[j] = *reinterpret_cast<const float*>(sv + r * ROW + 16 * L::v_chunk16(r, x / 4) + 4 * (x % 4));
+        }
+      } else {
+        const int x = 16 * t + 4 * (c16 % 4);
+        i16x4 w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = 16 * j + 4 * g + c16 / 4;
+          w[j] = read_columns(sv + r * ROW + 16 * L::v_chunk16(r, x / 8) + 2 * (x % 8));
+        }
+        f = __builtin_bit_cast(Frag, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      return f;
+    };
+    if (!careful) {
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        const Frag f = columns(t);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) o[n][t] = Mat<T>::mma16(f, fp[n], o[n][t]);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        const Frag f = columns(t);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) o[n][t] = Mat<T>::mma16(finite_only<T>(f), fp[n], o[n][t]);
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind)
+#pragma unroll
+          for (int n = 0; n < NC; ++n) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = k0 + 16 * (j / 4) + 4 * g + j % 4 < q[n].lim ? 1.0f : 0.0f;
+            const f32x4 hit = Mat<T>::mma16(odd_ones<T>(f, kind), to_frag<T>(v), f32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][t][i] += hit[i] > 0.0f ? odd_value(kind) : 0.0f;
+          }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // join of the four waves
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    l[n] += __shfl_xor(l[n], 16);
+    l[n] += __shfl_xor(l[n], 32);
+    if (g == 0) sm[wave][16 * n + c16] = m[n], sl[wave][16 * n + c16] = l[n];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    float top = a.floor, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][16 * n + c16]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      sum += sl[w][16 * n + c16] * __builtin_amdgcn_exp2f((sm[w][16 * n + c16] - top) * a.exp_by);
+    const float by = __builtin_amdgcn_exp2f((m[n] - top) * a.exp_by);
+    if (n) __syncthreads();
+    f32x4* mine = reinterpret_cast<f32x4*>(sv);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      f32x4 v = o[n][t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = l[n] == 0.0f ? 0.0f : v[i] * by;  // an unused wave adds nothing
+      mine[t * kWave + lane] = v;
+    }
+    __syncthreads();
+    if (16 * n + c16 < cols) {
+      const int64_t part = (int64_t)blockIdx.x * a.n_q * a.heads + row[n];
+      if (a.splits > 1 && wave == 0 && g == 0) a.part_ml[part] = f32x2{top, sum};
+      const float inv = 1.0f / sum;
+      for (int t = wave; t < D / 16; t += 4) {
+        const int x = 16 * t + 4 * g;
+        if (x >= a.d) continue;
+        f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v += reinterpret_cast<const f32x4*>(strips[w])[t * kWave + lane];
+        if (a.splits > 1) {
+          const float r[4] = {v[0], v[1], v[2], v[3]};
+          if (sum != 0.0f) store4(a.part_o + part * a.d + x, r);
+        } else {
+          float r[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = sum == 0.0f ? 0.0f : v[i] * inv;
+          const int64_t i = row[n] / a.heads, head = row[n] % a.heads;
+          store4(static_cast<T*>(a.out) + i * a.out_row + head * a.out_head + x, r);
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t rows_t(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)a.splits, (unsigned)a.kv_heads, (unsigned)a.n_docs);
+#define SPC_D(D, NC) hipLaunchKernelGGL((k_attn_rows<T, D, NC>), grid, dim3(256), 0, s, a)
+#define SPC_C(D)                      \
+  do {                                \
+    if (p.cols <= 16) SPC_D(D, 1);      \
+    else if (p.cols <= 32) SPC_D(D, 2); \
+    else SPC_D(D, 4);                   \
+  } while (0)
+  if (a.d <= 32) SPC_C(32);
+  else if (a.d <= 64) SPC_C(64);
+  else if (a.d <= 128) SPC_C(128);
+  else SPC_C(256);
+#undef SPC_C
+#undef SPC_D
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_rows(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
+  if (dtype == 0) return rows_t<float>(a, p, s);
+  if (dtype == 1) return rows_t<_Float16>(a, p, s);
+  return rows_t<__bf16>(a, p, s);
+}
+
+}  // namespace spc

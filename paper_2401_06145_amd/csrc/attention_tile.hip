@@ -1,0 +1,322 @@
+// Attention with many queries per document: whole prompts and scenes.
+#include "attention_device.h"
+
+namespace spc {
+namespace {
+using namespace attn;
+
+// What the scores go through.  kBare: nothing but their scale.  kCapped: a cap of at most 60
+// and no bias, in types of float32's exponent range: exp(score) itself lies between e^-60 and
+// e^60, so there is no running maximum to keep.  kAny: everything else.
+enum Mode { kBare, kCapped, kAny };
+constexpr float kCapWithoutMaximum = 60.0f;
+
+// 16 bytes a lane from memory straight into LDS, P times: those at `at[i]` of the `bytes` that
+// begin at `from` (zeros where they end before) to the wave's 1024 bytes at `to` + 4096 i.
+template <int P>
+__device__ __forceinline__ void bring_rows(const char* from, int bytes, char* to, const int* at) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, bytes, 0x00020000);
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + 4096 * i), 16, at[i], 0, 0, 0);
+}
+
+// A workgroup of four waves takes 128 queries of one head and one range of keys, KT keys at a
+// time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
+// from memory straight into the other half of LDS while one is multiplied.
+//
+// Workgroups with the same key head are neighbours in time on one XCD (workgroups go around
+// the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
+// where the call is causal) start first.
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256, D * sizeof(T) <= 256 ? 2 : 1) void k_attn_tile(AttnArgs a) {
+  typedef typename Mat<T>::Frag Frag;
+  constexpr int QT = kQueryTile, E = sizeof(T), ROW = D * E;
+  constexpr int KT = ROW >= 1024 ? 32 : 64;
+  typedef Lds<ROW> L;
+  constexpr int P = KT * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
+  __shared__ __align__(16) char sk[2][KT * ROW], sv[2][KT * ROW];
+  __shared__ f32x4 spos[2][KT];
+  __shared__ uint32_t odd_at[3 * KT * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
+
+  // which slot, head and range of keys
+  const int per = a.heads * a.slots, split = blockIdx.x / per, in = blockIdx.x - split * per;
+  const int h = in % a.heads, head = a.heads % 8 == 0 ? h % 8 * (a.heads / 8) + h / 8 : h;
+  const int slot = a.slots - 1 - in / a.heads;
+  int first;
+  const int doc = find_doc(a, slot, QT, &first);
+  const Doc d = load_doc(a, doc);
+  const int i0 = (slot - first) * QT;
+  if (i0 >= d.len_q) return;
+  const int kvh = head / (a.heads / a.kv_heads);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = threadIdx.x % kWave, c32 = lane % 32, half = lane / 32;
+
+  // the rows of this wave, and what they see
+  const int row = i0 + wave * 32 + c32;
+  const Query q = make_query(a, d, std::min(row, d.len_q - 1), head);
+  Frag fq[D / 16];
+  {
+    const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + std::min(row, d.len_q - 1)) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const int at = 16 * k + 8 * half;
+      fq[k] = at < a.d ? load_frag(p + at) : zero_frag<T>();
+    }
+  }
+  const int wave_i0 = std::min(i0 + wave * 32, d.len_q - 1);
+  const int lim_lo = seen(a, d, wave_i0), lim_hi = seen(a, d, std::min(wave_i0 + 31, d.len_q - 1));
+  const int tile_lo = seen(a, d, i0), tile_hi = seen(a, d, std::min(i0 + QT, d.len_q) - 1);
+  const int k_begin = split * a.chunk, k_end = std::min(tile_hi, k_begin + a.chunk);
+
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+  float m = MODE == kCapped ? 0.0f : a.floor, l = 0.0f;
+
+  // A thread's chunks of a tile: 16 bytes that lie in LDS where the wave's lanes follow each
+  // other, and in memory where the exchanged order puts them.  Columns that do not exist lie
+  // out of the buffer's range, which gives zeros, as do rows behind the last key.
+  const char* kp = static_cast<const char*>(a.k) + (d.k0 * a.k_row + (int64_t)kvh * a.k_head) * E;
+  const char* vp = static_cast<const char*>(a.v) + (d.k0 * a.v_row + (int64_t)kvh * a.v_head) * E;
+  const int k_bytes = (int)a.k_row * E, v_bytes = (int)a.v_row * E;
+  int at_k[P], at_v[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const uint32_t p = (4 * i + wave) * kWave + lane, r = p / L::CH, c = p % L::CH;
+    const int ck = L::k_chunk(r, c), cv = L::v_chunk(r, c);
+    at_k[i] = ck * (16 / E) < a.d ? r * k_bytes + 16 * ck : INT32_MIN;
+    at_v[i] = cv * (16 / E) < a.d ? r * v_bytes + 16 * cv : INT32_MIN;
+  }
+  const auto bring = [&](int k0, int b) {
+    const int rows = std::min(d.len_k - k0, KT);
+    bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
+    bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
+  };
+  const auto voxel = [&](int k0) {
+    f32x4 p = {0, 0, 0, 0};
+    if (MODE == kAny && a.k_pos && threadIdx.x < KT && k0 + (int)threadIdx.x < d.len_k) {
+      const int32_t* v = a.k_pos + 4 * (d.k0 + k0 + threadIdx.x);
+      p = f32x4{(float)v[1], (float)v[2], (float)v[3], 0};
+    }
+    return p;
+  };
+
+  if (k_begin < k_end) {
+    bring(k_begin, 0);
+    if (MODE == kAny && a.k_pos && threadIdx.x < KT) spos[0][threadIdx.x] = voxel(k_begin);
+  }
+  int b = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += KT, b ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile is in LDS
+    __syncthreads();                     // and so are the others'; the other half is free
+    // A hidden key's value is multiplied by 0, which must not make an infinity or a NaN of it
+    // part of the sum.  Where a tile with hidden keys has such values they leave the tile, and
+    // go to the queries that see them after the product.
+    bool odd = false;
+    if (k0 + KT > tile_lo) {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        odd |= odd_values<T>(*reinterpret_cast<const u32x4*>(sv[b] + 16 * (threadIdx.x + 256 * i)));
+      odd = __syncthreads_or(odd);
+      if (odd) {
+        for (int i = threadIdx.x; i < 3 * KT * (D / 32); i += 256) odd_at[i] = 0;
+        __syncthreads();
+        for (uint32_t p = threadIdx.x; p < KT * L::CH; p += 256) {
+          const int r = p / L::CH, x = L::v_chunk(r, p % L::CH) * (16 / E);
+          for (int j = 0; j < 16 / E; ++j) {
+            T* v = reinterpret_cast<T*>(sv[b] + 16 * p) + j;
+            const int kind = odd_kind((float)*v);
+            if (kind < 0) continue;
+            atomicOr(&odd_at[(kind * KT + r) * (D / 32) + (x + j) / 32], 1u << ((x + j) % 32));
+            *v = (T)0.0f;
+          }
+        }
+        __syncthreads();
+      }
+    }
+    f32x4 next_voxel;
+    if (k0 + KT < k_end) {
+      bring(k0 + KT, b ^ 1);
+      if (MODE == kAny) next_voxel = voxel(k0 + KT);
+    }
+    if (k0 < lim_hi) {  // else nothing for this wave
+      float s[KT / 2];
+      {
+        f32x16 acc[KT / 32];
+#pragma unroll
+        for (int h = 0; h < KT / 32; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[h][i] = 0.0f;
+#pragma unroll
+        for (int h = 0; h < KT / 32; ++h) {
+          const int r = 32 * h + c32;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            Frag f;
+            if constexpr (E == 4) {
+              const int c = 4 * k + 2 * half;
+              const f32x4 x = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c));
+              const f32x4 y = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c + 1));
+              f = f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            } else {
+              f = *reinterpret_cast<const Frag*>(sk[b] + r * ROW + 16 * L::k_chunk(r, 2 * k + half));
+            }
+            acc[h] = Mat<T>::mma32(f, fq[k], acc[h]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < KT / 2; ++i) s[i] = acc[i / 16][i % 16];
+      }
+      const bool masked = k0 + KT > lim_lo;
+      const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
+      if constexpr (MODE == kCapped) {
+        // exp(cap tanh(u)) by way of tanh(u) = 1 - 2 / (1 + e^{2u})
+#pragma unroll
+        for (int i = 0; i < KT / 2; ++i) {
+          const float e = __builtin_amdgcn_exp2f(s[i] * a.tanh_by);
+          s[i] = __builtin_amdgcn_exp2f(fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + e), a.cap_log2));
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < KT / 2; ++i) s[i] = k0 + at(i) < q.lim ? s[i] : 0.0f;
+        }
+      } else {
+        if constexpr (MODE == kAny) {
+          to_scores<KT / 2>(a, q, s, masked, [&](int i) { return k0 + at(i); }, [&](int i) { return spos[b][at(i)]; });
+        } else if (masked) {
+#pragma unroll
+          for (int i = 0; i < KT / 2; ++i) s[i] = k0 + at(i) < q.lim ? s[i] : -INFINITY;
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < KT / 2; ++i) top = fmaxf(top, s[i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m)) {
+          const float by = __builtin_amdgcn_exp2f((m - top) * a.exp_by);
+          l *= by;
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= by;
+          m = top;
+        }
+        const float off = m * a.exp_by;
+#pragma unroll
+        for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.exp_by, -off));
+      }
+      {
+        float sum[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int i = 4; i < KT / 2; ++i) sum[i % 4] += s[i];
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+      Frag fp[KT / 16];
+#pragma unroll
+      for (int c = 0; c < KT / 16; ++c) fp[c] = to_frag<T>(s + 8 * c);
+
+      // columns of V: fragment (t, c) of out^T's rows 32 t .. and keys 16 c + {4 half + j, 8 + 4 half + j}
+      const auto columns = [&](int t, int c) {
+        Frag f;
+        if constexpr (E == 4) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 16 * c + 8 * (j / 4) + 4 * half + j % 4, x = 32 * t + c32;
+            f[j] = *reinterpret_cast<const float*>(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 4) + 4 * (x % 4));
+          }
+        } else {
+          const int i = lane % 16, x = 32 * t + 16 * (lane / 16 % 2) + 4 * (i % 4);
+          i16x4 w[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = 16 * c + 8 * j + 4 * half + i / 4;
+            w[j] = read_columns(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 8) + 2 * (x % 8));
+          }
+          f = __builtin_bit_cast(Frag, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return f;
+      };
+#pragma unroll
+      for (int c = 0; c < KT / 16; ++c)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) o[t] = Mat<T>::mma32(columns(t, c), fp[c], o[t]);
+      if (odd) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll 1
+          for (int kr = 0; kr < 3 * KT; ++kr) {
+            const uint32_t bits = odd_at[kr * (D / 32) + t];
+            if (bits == 0 || k0 + kr % KT >= q.lim) continue;
+            const float v = odd_value(kr / KT);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] += bits >> (8 * (i / 4) + 4 * half + i % 4) & 1 ? v : 0.0f;
+          }
+      }
+    }
+    if (MODE == kAny && a.k_pos && threadIdx.x < KT && k0 + KT < k_end) spos[b ^ 1][threadIdx.x] = next_voxel;
+  }
+
+  const float sum = l + __shfl_xor(l, 32);
+  if (row >= d.len_q) return;
+  const int64_t out_at = (int64_t)(d.q0 + row) * a.heads + head;
+  if (a.splits > 1) {
+    const int64_t part = (int64_t)split * a.n_q * a.heads + out_at;
+    if (half == 0) a.part_ml[part] = f32x2{m, sum};
+    if (sum == 0.0f) return;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int x = 32 * t + 8 * (i / 4) + 4 * half;
+        const float v[4] = {o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+        if (x < a.d) store4(a.part_o + part * a.d + x, v);
+      }
+  } else {
+    const float by = 1.0f / sum;
+    T* out = static_cast<T*>(a.out) + (int64_t)(d.q0 + row) * a.out_row + (int64_t)head * a.out_head;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int x = 32 * t + 8 * (i / 4) + 4 * half;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = sum == 0.0f ? 0.0f : o[t][i + j] * by;
+        if (x < a.d) store4(out + x, v);
+      }
+  }
+}
+
+template <typename T, int MODE>
+void tile_mode(const AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.heads * a.slots * a.splits));
+#define SPC_D(D) hipLaunchKernelGGL((k_attn_tile<T, D, MODE>), grid, dim3(256), 0, s, a)
+  if (a.d <= 32) SPC_D(32);
+  else if (a.d <= 64) SPC_D(64);
+  else if (a.d <= 128) SPC_D(128);
+  else SPC_D(256);
+#undef SPC_D
+}
+
+template <typename T>
+void tile_t(const AttnArgs& a, hipStream_t s) {
+  if (a.cap == 0.0f && !a.slopes) return tile_mode<T, kBare>(a, s);
+  if constexpr (!std::is_same_v<T, _Float16>) {
+    if (!a.slopes && a.cap <= kCapWithoutMaximum) return tile_mode<T, kCapped>(a, s);
+  }
+  tile_mode<T, kAny>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
+  if ((int64_t)a.heads * p.slots * p.splits > 0x7fffffff) return hipErrorInvalidValue;
+  if (dtype == 0) tile_t<float>(a, s);
+  else if (dtype == 1) tile_t<_Float16>(a, s);
+  else tile_t<__bf16>(a, s);
+  return hipGetLastError();
+}
+
+}  // namespace spc
