@@ -173,12 +173,9 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 256 ? 2 : 1) void k_attn_tile
       const bool masked = k0 + KT > lim_lo;
       const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
       if constexpr (MODE == kCapped) {
-        // exp(cap tanh(u)) by way of tanh(u) = 1 - 2 / (1 + e^{2u})
+        cap_scores<KT / 2>(a, s);
 #pragma unroll
-        for (int i = 0; i < KT / 2; ++i) {
-          const float e = __builtin_amdgcn_exp2f(s[i] * a.tanh_by);
-          s[i] = __builtin_amdgcn_exp2f(fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + e), a.cap_log2));
-        }
+        for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
         if (masked) {
 #pragma unroll
           for (int i = 0; i < KT / 2; ++i) s[i] = k0 + at(i) < q.lim ? s[i] : 0.0f;
