@@ -13,13 +13,32 @@ constexpr float kCapWithoutMaximum = 60.0f;
 
 // 16 bytes a lane from memory straight into LDS, P times: those at `at[i]` of the `bytes` that
 // begin at `from` (zeros where they end before) to the wave's 1024 bytes at `to` + 4096 i.
+// Written as assembly because of the waits: of the builtin's loads the compiler awaits the
+// tile under way before it reads the tile that is there.  The caller waits (vmcnt) itself.
 template <int P>
 __device__ __forceinline__ void bring_rows(const char* from, int bytes, char* to, const int* at) {
-  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, bytes, 0x00020000);
+  const uint64_t base = reinterpret_cast<uint64_t>(from);
+  const u32x4 rsrc = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base),
+                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu),
+                      (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to;
 #pragma unroll
-  for (int i = 0; i < P; ++i)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + 4096 * i), 16, at[i], 0, 0, 0);
+  for (int i = 0; i < P; ++i) {
+    uint32_t kept;  // M0 holds the LDS address
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(kept)
+        : "s"(__builtin_amdgcn_readfirstlane(lds + 4096 * i)), "v"(at[i]), "s"(rsrc)
+        : "memory");
+  }
 }
+
+// Workgroups a CU holds, by the registers that rows of this many bytes need.
+constexpr int waves_a_simd(int row) { return row <= 64 ? 4 : row <= 128 ? 3 : row <= 256 ? 2 : 1; }
 
 // A workgroup of four waves takes 128 queries of one head and one range of keys, KT keys at a
 // time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
@@ -29,10 +48,16 @@ __device__ __forceinline__ void bring_rows(const char* from, int bytes, char* to
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
 // where the call is causal) start first.
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, D * sizeof(T) <= 256 ? 2 : 1) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
   constexpr int QT = kQueryTile, E = sizeof(T), ROW = D * E;
   constexpr int KT = ROW >= 1024 ? 32 : 64;
+  // Rows of 256 bytes leave registers for operands ahead of their use: all of a tile of K before
+  // the first product, a strip of V while the exponentials are computed (784 -> 770 us on whole
+  // documents of 128 columns; with distances, or 2 strips, the registers spill; shorter
+  // rows gain nothing).
+  constexpr bool AHEAD = ROW == 256 && MODE != kAny;
+  constexpr int VA = AHEAD ? 1 : 0;
   typedef Lds<ROW> L;
   constexpr int P = KT * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
   __shared__ __align__(16) char sk[2][KT * ROW], sv[2][KT * ROW];
@@ -150,26 +175,67 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 256 ? 2 : 1) void k_attn_tile
         for (int h = 0; h < KT / 32; ++h)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[h][i] = 0.0f;
-#pragma unroll
-        for (int h = 0; h < KT / 32; ++h) {
+        const auto key_rows = [&](int h, int k) {
           const int r = 32 * h + c32;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            Frag f;
-            if constexpr (E == 4) {
-              const int c = 4 * k + 2 * half;
-              const f32x4 x = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c));
-              const f32x4 y = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c + 1));
-              f = f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            } else {
-              f = *reinterpret_cast<const Frag*>(sk[b] + r * ROW + 16 * L::k_chunk(r, 2 * k + half));
-            }
-            acc[h] = Mat<T>::mma32(f, fq[k], acc[h]);
+          if constexpr (E == 4) {
+            const int c = 4 * k + 2 * half;
+            const f32x4 x = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c));
+            const f32x4 y = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c + 1));
+            return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+          } else {
+            return *reinterpret_cast<const Frag*>(sk[b] + r * ROW + 16 * L::k_chunk(r, 2 * k + half));
           }
+        };
+        if constexpr (AHEAD) {
+          Frag f[KT / 32][D / 16];
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int h = 0; h < KT / 32; ++h) f[h][k] = key_rows(h, k);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int h = 0; h < KT / 32; ++h) acc[h] = Mat<T>::mma32(f[h][k], fq[k], acc[h]);
+        } else {
+#pragma unroll
+          for (int h = 0; h < KT / 32; ++h)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) acc[h] = Mat<T>::mma32(key_rows(h, k), fq[k], acc[h]);
         }
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = acc[i / 16][i % 16];
       }
+      // columns of V: fragment (t, c) of out^T's rows 32 t .. and keys 16 c + {4 half + j, 8 + 4 half + j}
+      const auto columns = [&](int t, int c) {
+        Frag f;
+        if constexpr (E == 4) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 16 * c + 8 * (j / 4) + 4 * half + j % 4, x = 32 * t + c32;
+            f[j] = *reinterpret_cast<const float*>(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 4) + 4 * (x % 4));
+          }
+        } else {
+          const int i = lane % 16, x = 32 * t + 16 * (lane / 16 % 2) + 4 * (i % 4);
+          i16x4 w[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = 16 * c + 8 * j + 4 * half + i / 4;
+            w[j] = read_columns(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 8) + 2 * (x % 8));
+          }
+          f = __builtin_bit_cast(Frag, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return f;
+      };
+      Frag fv[D / 32][VA + 1];
+      if constexpr (VA > 0) {
+#pragma unroll
+        for (int c = 0; c < VA; ++c)
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t) fv[t][c] = columns(t, c);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+
       const bool masked = k0 + KT > lim_lo;
       const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
       if constexpr (MODE == kCapped) {
@@ -214,31 +280,12 @@ __global__ __launch_bounds__(256, D * sizeof(T) <= 256 ? 2 : 1) void k_attn_tile
 #pragma unroll
       for (int c = 0; c < KT / 16; ++c) fp[c] = to_frag<T>(s + 8 * c);
 
-      // columns of V: fragment (t, c) of out^T's rows 32 t .. and keys 16 c + {4 half + j, 8 + 4 half + j}
-      const auto columns = [&](int t, int c) {
-        Frag f;
-        if constexpr (E == 4) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = 16 * c + 8 * (j / 4) + 4 * half + j % 4, x = 32 * t + c32;
-            f[j] = *reinterpret_cast<const float*>(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 4) + 4 * (x % 4));
-          }
-        } else {
-          const int i = lane % 16, x = 32 * t + 16 * (lane / 16 % 2) + 4 * (i % 4);
-          i16x4 w[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = 16 * c + 8 * j + 4 * half + i / 4;
-            w[j] = read_columns(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 8) + 2 * (x % 8));
-          }
-          f = __builtin_bit_cast(Frag, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-        return f;
-      };
 #pragma unroll
       for (int c = 0; c < KT / 16; ++c)
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) o[t] = Mat<T>::mma32(columns(t, c), fp[c], o[t]);
+        for (int t = 0; t < D / 32; ++t) {
+          o[t] = Mat<T>::mma32(c < VA ? fv[t][c < VA ? c : 0] : columns(t, c), fp[c], o[t]);
+        }
       if (odd) {
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
