@@ -1170,6 +1170,8 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
   if (ld_x < k || ld_w < k || ld_y < n || ld_x_scale < kb || ld_w_scale < kb)
     return fail(SPCONV_EINVAL, "row stride shorter than a row");
   if (m > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (ld_x > kMostLinearStride || ld_w > kMostLinearStride || ld_x_scale > kMostLinearStride / 4)
+    return fail(SPCONV_EUNSUPPORTED, "rows of d_x, d_w and d_x_scale at most 8 MiB apart");
   if (m == 0 || n == 0) return SPCONV_OK;
   if (!d_y || (k > 0 && (!d_x || !d_x_scale || !d_w || !d_w_scale))) return fail(SPCONV_EINVAL, "NULL pointer");
   if (misaligned16(d_x) || misaligned16(d_w)) return fail(SPCONV_EINVAL, "d_x and d_w must be 16-byte aligned");

@@ -308,7 +308,9 @@ hipError_t launch_conv_small(const void* x, int64_t n_in, const void* w, const i
 hipError_t launch_rms_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* gamma, void* sum,
                            int64_t ld_sum, void* y, int64_t ld_y, float* scales, int64_t ld_scales, int64_t n, int c,
                            int dtype, bool bits8, float eps, hipStream_t s);
-// linear8.hip: e4m3 rows times e4m3 weights [n][k], scaled by blocks of 128.
+// linear8.hip: e4m3 rows times e4m3 weights [n][k], scaled by blocks of 128.  A tile's 256 rows
+// are addressed with 31 bits.
+constexpr int64_t kMostLinearStride = 1 << 23;
 hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, int64_t ld_xs, const void* w, int64_t ld_w,
                                 const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
                                 int relu, bool exact, hipStream_t s);

@@ -25,7 +25,8 @@ struct LinearArgs {
   int64_t m;
   int n, k, kb;  // kb: blocks of 128 columns
   int relu;
-  int wide_y;  // rows of y take 16-byte stores
+  int wide_y;   // rows of y take 16-byte stores
+  int wide_xs;  // rows of xs take 16-byte loads
 };
 
 // Eight e4m3 numbers as float16, exactly.
@@ -46,9 +47,8 @@ __device__ __forceinline__ f32x4 mma128(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1) 
   if constexpr (!EXACT) {
     const i32x8 a = __builtin_bit_cast(i32x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
     const i32x8 b = __builtin_bit_cast(i32x8, __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7));
-    // both operands e4m3, hardware scales 2^0 (127 in each byte)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0,
-                                                            0x7f7f7f7f);
+    // both operands e4m3; no hardware scales
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
   } else {
     f32x4 t = {0, 0, 0, 0};
 #pragma unroll
@@ -90,45 +90,108 @@ __device__ __forceinline__ void store_y(const LinearArgs& a, int64_t row, int n0
 }
 
 // ---------------------------------------------------------------------------
-// Tiles: a workgroup of WM x WN waves takes BM rows and BN outputs, a block of 128
-// columns at a time through LDS.  Rows of 128 bytes; the 16-byte chunk c of row r lies at
-// chunk c ^ (r / 2 % 8), so that 16 lanes reading one chunk of 16 rows meet every bank once.
+// Tiles: a workgroup of WM x WN waves takes BM rows and BN outputs, a block of 128 columns at
+// a time through LDS.  The next block of rows, weights and row scales is on its way from
+// memory straight into the other half of LDS while one is multiplied.  Rows of 128 bytes: the
+// 16-byte chunk c of row r lies at chunk c ^ (r / 2 % 8), so that 16 lanes reading one chunk
+// of 16 rows meet every bank once.
 // ---------------------------------------------------------------------------
+
+// WORDS times 4 bytes a lane from memory straight into LDS: those at `at` of the buffer (zeros
+// outside of it) to where the wave's lanes follow each other from `to` on.  The caller waits
+// (vmcnt); the compiler would await loads under way before every read of LDS.
+template <int WORDS>
+__device__ __forceinline__ void bring(u32x4 rsrc, int at, const void* to) {
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)to);
+  uint32_t kept;  // M0 holds the LDS address
+  if constexpr (WORDS == 4)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds), "v"(at), "s"(rsrc) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "s"(lds), "v"(at), "s"(rsrc) : "memory");
+}
+__device__ __forceinline__ u32x4 buffer(const void* from, int64_t bytes) {
+  const uint64_t base = reinterpret_cast<uint64_t>(from);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
+}
+
 template <typename T, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs a) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(LinearArgs a) {
   constexpr int TH = 64 * WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
-  constexpr int PX = BM * 8 / TH, PW = BN * 8 / TH;  // 16-byte chunks a thread stages
-  __shared__ __align__(16) u32x4 sx[BM * 8], sw[BN * 8];
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  constexpr int PX = BM * 8 / TH, PW = BN * 8 / TH;  // 16-byte chunks a thread brings
+  static_assert(TH >= BM, "a thread brings at most one row scale");
+  __shared__ __align__(16) u32x4 sx[2][BM * 8], sw[2][BN * 8];
+  __shared__ __align__(16) float sxs[2][BM * 4];  // row scales of four blocks
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int wm = wave / WN, wn = wave % WN;
   const int r16 = lane % 16, g = lane / 16;
-  const int64_t m0 = (int64_t)blockIdx.y * BM;
-  const int n0 = blockIdx.x * BN;
 
-  const uint8_t* px[PX];
-  const uint8_t* pw[PW];
-  int sat_x[PX], sat_w[PW];
+  // Workgroups go around the 8 XCDs: each takes a run of tiles, in columns of 4 tiles of rows,
+  // so that the 32 under way share rows and weights in its L2.
+  const int tiles_m = (int)((a.m + BM - 1) / BM), tiles_n = (a.n + BN - 1) / BN;
+  const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8, each = total / 8, rest = total % 8;
+  const int tile = xcd * each + std::min(xcd, rest) + blockIdx.x / 8;
+  const int strip = tile / (4 * tiles_n) * 4, high = std::min(4, tiles_m - strip), in = tile - strip * tiles_n;
+  const int64_t m0 = (int64_t)(strip + in % high) * BM;
+  const int n0 = in / high * BN;
+
+  const int rows = (int)std::min<int64_t>(a.m - m0, BM), outs = std::min(a.n - n0, BN);
+  const uint8_t* x = a.x + m0 * a.ld_x;
+  const uint8_t* w = a.w + (int64_t)n0 * a.ld_w;
+  int at_x[PX], at_w[PW];
 #pragma unroll
   for (int i = 0; i < PX; ++i) {
-    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8;
-    px[i] = a.x + std::min<int64_t>(m0 + r, a.m - 1) * a.ld_x + 16 * c;
-    sat_x[i] = r * 8 + (c ^ (r / 2 % 8));
+    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8 ^ r / 2 % 8;
+    at_x[i] = r < rows ? r * (int)a.ld_x + 16 * c : INT32_MIN;
   }
   // LDS row 16 t + 4 q + b of a wave's weights holds output 4 NT q + 4 t + b, so that a lane
   // ends with 4 NT consecutive outputs of its row
 #pragma unroll
   for (int i = 0; i < PW; ++i) {
-    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8;
-    const int in = r % (16 * NT), out = r - in + 4 * NT * (in / 4 % 4) + 4 * (in / 16) + in % 4;
-    pw[i] = a.w + (int64_t)std::min(n0 + out, a.n - 1) * a.ld_w + 16 * c;
-    sat_w[i] = r * 8 + (c ^ (r / 2 % 8));
+    const int p = threadIdx.x + TH * i, r = p / 8, c = p % 8 ^ r / 2 % 8;
+    const int in_wave = r % (16 * NT), out = r - in_wave + 4 * NT * (in_wave / 4 % 4) + 4 * (in_wave / 16) + in_wave % 4;
+    at_w[i] = out < outs ? out * (int)a.ld_w + 16 * c : INT32_MIN;
   }
-  const float* xs[MT];
+  const int at_s = (int)threadIdx.x < rows ? (int)threadIdx.x * (int)a.ld_xs * 4 : INT32_MIN;
+  const int by_row = a.wide_xs ? 4 : 1, by_block = a.wide_xs ? 1 : BM;
+  // constant memory: a scalar load, which does not wait for the tiles under way as a vector load would
+  const auto ws = (const __attribute__((address_space(4))) float*)(
+      a.ws + (int64_t)std::min((n0 + wn * 16 * NT) / kScaleBlock, (a.n - 1) / kScaleBlock) * a.ld_ws);
+
+  const auto bring_block = [&](int b, int buf) {
+    const int left = a.k - b * kScaleBlock;
+    const u32x4 rx = buffer(x + (int64_t)b * kScaleBlock, (int64_t)(rows - 1) * a.ld_x + std::min(left, kScaleBlock));
+    const u32x4 rw = buffer(w + (int64_t)b * kScaleBlock, (int64_t)(outs - 1) * a.ld_w + std::min(left, kScaleBlock));
+    if (left < kScaleBlock) {  // the last block: its missing columns are zeros
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-    xs[i] = a.xs + std::min<int64_t>(m0 + wm * 16 * MT + 16 * i + r16, a.m - 1) * a.ld_xs;
-  const float* ws = a.ws + (int64_t)std::min((n0 + wn * 16 * NT) / kScaleBlock, (a.n - 1) / kScaleBlock) * a.ld_ws;
+      for (int i = 0; i < PX; ++i) {
+        const int p = threadIdx.x + TH * i;
+        if (16 * (p % 8 ^ p / 16 % 8) >= left) at_x[i] = INT32_MIN;
+      }
+#pragma unroll
+      for (int i = 0; i < PW; ++i) {
+        const int p = threadIdx.x + TH * i;
+        if (16 * (p % 8 ^ p / 16 % 8) >= left) at_w[i] = INT32_MIN;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PX; ++i) bring<4>(rx, at_x[i], &sx[buf][TH * i + 64 * wave]);
+#pragma unroll
+    for (int i = 0; i < PW; ++i) bring<4>(rw, at_w[i], &sw[buf][TH * i + 64 * wave]);
+    if (b % 4 == 0 && 64 * wave < BM) {  // a row's scales of four blocks at once, where they are aligned
+      const u32x4 rs = buffer(a.xs + m0 * a.ld_xs + b, ((int64_t)(rows - 1) * a.ld_xs + a.kb - b) * 4);
+      if (a.wide_xs) {
+        bring<4>(rs, at_s, &sxs[b / 4 % 2][256 * wave]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bring<1>(rs, at_s + 4 * i, &sxs[b / 4 % 2][BM * i + 64 * wave]);
+      }
+    }
+  };
 
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -136,47 +199,44 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tile(LinearArgs a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
+  if (a.kb > 0) bring_block(0, 0);
   for (int b = 0; b < a.kb; ++b) {
-    const int left = a.k - b * kScaleBlock;  // columns of this block that exist
-    u32x4 vx[PX], vw[PW];
-#pragma unroll
-    for (int i = 0; i < PX; ++i) {
-      vx[i] = u32x4{0, 0, 0, 0};
-      if (16 * (int)((threadIdx.x + TH * i) % 8) < left)
-        vx[i] = *reinterpret_cast<const u32x4*>(px[i] + (int64_t)b * kScaleBlock);
-    }
-#pragma unroll
-    for (int i = 0; i < PW; ++i) {
-      vw[i] = u32x4{0, 0, 0, 0};
-      if (16 * (int)((threadIdx.x + TH * i) % 8) < left)
-        vw[i] = *reinterpret_cast<const u32x4*>(pw[i] + (int64_t)b * kScaleBlock);
-    }
+    const int buf = b & 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the block is in LDS
+    __syncthreads();                     // and so are the others'; the other half is free
+    if (b + 1 < a.kb) bring_block(b + 1, buf ^ 1);
     const float sb = ws[b];
-    float scale[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) scale[i] = xs[i][b] * sb;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PX; ++i) sx[sat_x[i]] = vx[i];
-#pragma unroll
-    for (int i = 0; i < PW; ++i) sw[sat_w[i]] = vw[i];
-    __syncthreads();
     u32x4 fw[NT][2];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int r = wn * 16 * NT + 16 * j + r16;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) fw[j][h] = sw[r * 8 + ((2 * g + h) ^ (r / 2 % 8))];
+      for (int h = 0; h < 2; ++h) fw[j][h] = sw[buf][r * 8 + ((2 * g + h) ^ (r / 2 % 8))];
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
+    // the products of one strip of 16 rows are scaled and added while the next one's are formed
+    f32x4 t[2][NT];
+    float scale[2];
+    u32x4 f[2][2];
+    const auto rows_of = [&](int i) {
       const int r = wm * 16 * MT + 16 * i + r16;
-      const u32x4 f0 = sx[r * 8 + ((2 * g) ^ (r / 2 % 8))], f1 = sx[r * 8 + ((2 * g + 1) ^ (r / 2 % 8))];
+      f[i & 1][0] = sx[buf][r * 8 + ((2 * g) ^ (r / 2 % 8))];
+      f[i & 1][1] = sx[buf][r * 8 + ((2 * g + 1) ^ (r / 2 % 8))];
+    };
+    rows_of(0);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const f32x4 t = mma128<EXACT>(fw[j][0], fw[j][1], f0, f1);
+    for (int i = 0; i <= MT; ++i) {
+      if (i + 1 < MT) rows_of(i + 1);
+      if (i < MT) {
+        scale[i & 1] = sxs[b / 4 % 2][by_row * (wm * 16 * MT + 16 * i + r16) + by_block * (b % 4)] * sb;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(scale[i], t[e], acc[i][j][e]);
+        for (int j = 0; j < NT; ++j) t[i & 1][j] = mma128<EXACT>(fw[j][0], fw[j][1], f[i & 1][0], f[i & 1][1]);
+      }
+      if (i > 0) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i > 0 ? i - 1 : 0][j][e] = fmaf(scale[(i & 1) ^ 1], t[(i & 1) ^ 1][j][e], acc[i > 0 ? i - 1 : 0][j][e]);
       }
     }
   }
@@ -255,14 +315,18 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
 #undef SPC_R
     return;
   }
-  const dim3 grid((unsigned)((a.n + 127) / 128), (unsigned)((a.m + 127) / 128));
+#define SPC_T(EXACT, BM, BN, WM, WN)                                                                                  \
+  hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN>),                                                       \
+                     dim3((unsigned)(((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN))), dim3(64 * WM * WN), 0, s, a)
   if constexpr (!std::is_same_v<T, float>) {
     if (!exact) {
-      hipLaunchKernelGGL((k_linear_tile<T, false, 128, 128, 2, 2>), grid, dim3(256), 0, s, a);
+      if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4);
+      else SPC_T(false, 128, 128, 2, 2);
       return;
     }
   }
-  hipLaunchKernelGGL((k_linear_tile<T, true, 128, 128, 2, 2>), grid, dim3(256), 0, s, a);
+  SPC_T(true, 128, 128, 2, 2);
+#undef SPC_T
 }
 
 }  // namespace
@@ -271,11 +335,12 @@ hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, in
                                 const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
                                 int relu, bool exact, hipStream_t s) {
   if (m <= 0 || n <= 0) return hipSuccess;
-  if ((m + 127) / 128 > 65535) return hipErrorInvalidValue;
+  if (((m + 127) / 128) * ((n + 127) / 128) > 0x7fffffff) return hipErrorInvalidValue;
   ProfScope ps(KN_SCALED_LINEAR, s);
   const int64_t e = dtype == 0 ? 4 : 2;
   LinearArgs a = {static_cast<const uint8_t*>(x), xs, static_cast<const uint8_t*>(w), ws, y, ld_x, ld_xs, ld_w, ld_ws,
-                  ld_y, m, n, k, (k + kScaleBlock - 1) / kScaleBlock, relu, 0};
+                  ld_y, m, n, k, (k + kScaleBlock - 1) / kScaleBlock, relu, 0, 0};
+  a.wide_xs = reinterpret_cast<uintptr_t>(xs) % 16 == 0 && ld_xs % 4 == 0;
   a.wide_y = reinterpret_cast<uintptr_t>(y) % 16 == 0 && ld_y * e % 16 == 0;
   if (dtype == 0) linear_t<float>(a, true, s);
   else if (dtype == 1) linear_t<_Float16>(a, exact, s);

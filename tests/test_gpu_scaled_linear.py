@@ -117,3 +117,17 @@ def test_quantized_weights():
     f = s.double().repeat_interleave(128, 0)[:200].repeat_interleave(128, 1)[:, :300]
     step = torch.maximum(w.double().abs() * 2.0 ** -4, f * 2.0 ** -10)
     assert bool(((q.float().double() * f - w.double()).abs() <= step * (1 + 2.0 ** -10)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(4100, 4200, 272), (4352, 4096, 1152), (8191, 2100, 640)])
+def test_linear_of_many_tiles(m, n, k, dtype):
+    """Large products take tiles of 256 x 256."""
+    say(f"scaled product {m} x {n} x {k} {dtype}")
+    x, w = bits8(m, k, 21), bits8(n, k, 22)
+    xs, ws = scales(m, k, 23) * 1e-4, scales(-(-n // 128), k, 24) * 1e-4
+    want, mag = ref.scaled_linear(x, xs, w, ws)
+    got = B.scaled_linear(x, xs, w, ws, dtype)
+    bound = mag * (7 * 2.0 ** -13 + (min(k, 128) + k / 128 + 4) * 2.0 ** -24) + want.abs() * ref.UNIT[dtype] + ref.TINY[dtype]
+    assert bool(((got.double() - want).abs() <= bound).all())
+    ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "exact")
