@@ -260,69 +260,118 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(LinearArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: a workgroup takes 16 outputs and all rows (16 MT of them); its waves share the
-// blocks of 128 columns out among themselves and add their sums through LDS at the end.
-// Weights go from memory straight into registers: a matrix operand's lane reads 32
-// consecutive bytes of its row, four lanes a whole 128-byte line.
+// Few rows: a workgroup takes 16 NT outputs and 16 MT rows; its waves share the blocks of 128
+// columns out among themselves and add their sums through LDS at the end, in the order of
+// the waves.  Operands go from memory straight into registers, up to 48 rows a block
+// ahead of their products: a matrix operand's lane reads 32 consecutive bytes of its row, four
+// lanes a whole 128-byte line.  What bounds it: the latency of a wave's two to four blocks, one
+// round trip to memory each.
 // ---------------------------------------------------------------------------
-template <typename T, int MT, int WAVES>
+template <typename T, int MT, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_rows(LinearArgs a) {
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int r16 = lane % 16, g = lane / 16;
-  const int n0 = blockIdx.x * 16;
-  const uint8_t* w = a.w + (int64_t)std::min(n0 + r16, a.n - 1) * a.ld_w + 32 * g;
-  const float* ws = a.ws + (int64_t)(n0 / kScaleBlock) * a.ld_ws;
+  const int n0 = blockIdx.x * 16 * NT;
+  const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
+  const uint8_t* w[NT];
   const uint8_t* x[MT];
   const float* xs[MT];
-  f32x4 acc[MT];
+  const float* ws = a.ws + (int64_t)(n0 / kScaleBlock) * a.ld_ws;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) w[j] = a.w + (int64_t)std::min(n0 + 16 * j + r16, a.n - 1) * a.ld_w + 32 * g;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int64_t row = std::min<int64_t>(16 * i + r16, a.m - 1);
+    const int64_t row = std::min<int64_t>(m0 + 16 * i + r16, a.m - 1);
     x[i] = a.x + row * a.ld_x + 32 * g;
     xs[i] = a.xs + row * a.ld_xs;
-    acc[i] = f32x4{0, 0, 0, 0};
   }
-  const u32x4 zero = {0, 0, 0, 0};
-  for (int b = wave; b < a.kb; b += WAVES) {
+  struct Block {
+    u32x4 w[NT][2], x[MT][2];
+    float xs[MT], ws;
+  };
+  const auto fetch = [&](int b, Block& k) {
     const int at = b * kScaleBlock;
-    const bool h0 = at + 32 * g < a.k, h1 = at + 32 * g + 16 < a.k;
-    const u32x4 w0 = h0 ? *reinterpret_cast<const u32x4*>(w + at) : zero;
-    const u32x4 w1 = h1 ? *reinterpret_cast<const u32x4*>(w + at + 16) : zero;
-    const float sb = ws[b];
+    const bool in[2] = {at + 32 * g < a.k, at + 32 * g + 16 < a.k};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        k.w[j][h] = in[h] ? *reinterpret_cast<const u32x4*>(w[j] + at + 16 * h) : u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        k.x[i][h] = in[h] ? *reinterpret_cast<const u32x4*>(x[i] + at + 16 * h) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) k.xs[i] = xs[i][b];
+    k.ws = ws[b];
+  };
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+  constexpr bool AHEAD = MT * NT <= 3;
+  Block now, next;
+  if (AHEAD && wave < a.kb) fetch(wave, now);
+  for (int b = wave; b < a.kb; b += WAVES) {
+    if (!AHEAD) fetch(b, now);
+    else if (b + WAVES < a.kb) fetch(b + WAVES, next);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const u32x4 x0 = h0 ? *reinterpret_cast<const u32x4*>(x[i] + at) : zero;
-      const u32x4 x1 = h1 ? *reinterpret_cast<const u32x4*>(x[i] + at + 16) : zero;
-      const float scale = xs[i][b] * sb;
-      const f32x4 t = mma128<true>(w0, w1, x0, x1);
+      const float by = now.xs[i] * now.ws;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(scale, t[e], acc[i][e]);
+      for (int j = 0; j < NT; ++j) {
+        const f32x4 t = mma128<true>(now.w[j][0], now.w[j][1], now.x[i][0], now.x[i][1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(by, t[e], acc[i][j][e]);
+      }
     }
+    if (AHEAD) now = next;
   }
-  __shared__ f32x4 part[WAVES][MT][kWave];
+  __shared__ f32x4 part[WAVES][MT * NT][kWave];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+  for (int i = 0; i < MT * NT; ++i) part[wave][i][lane] = acc[i / NT][i % NT];
   __syncthreads();
-  for (int i = wave; i < MT; i += WAVES) {
+  for (int i = wave; i < MT * NT; i += WAVES) {
     f32x4 v = part[0][i][lane];
 #pragma unroll
     for (int q = 1; q < WAVES; ++q) v += part[q][i][lane];
     float r[4] = {v[0], v[1], v[2], v[3]};
-    store_y<T, 4>(a, 16 * i + r16, n0 + 4 * g, r);
+    store_y<T, 4>(a, m0 + 16 * (i / NT) + r16, n0 + 16 * (i % NT) + 4 * g, r);
   }
+}
+
+// The few-row form reads every row for each 16 or 32 outputs, but shares out the columns: it
+// takes up to 64 rows, and more of them where the columns are many and one workgroup of
+// 64 rows x 32 outputs a CU does the whole (128 x 4096 x 4096 18.5 us against 26 of the tiles, 300 x
+// 1024 x 4096 18.0 against 26; two rounds take 33, and 8 blocks of columns are even).
+bool few_rows(const LinearArgs& a) {
+  return a.m <= 64 || (a.kb >= 24 && (a.m + 63) / 64 * ((a.n + 31) / 32) <= 256);
 }
 
 template <typename T>
 void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
-  if (a.m <= 64) {
-    const dim3 grid((unsigned)((a.n + 15) / 16));
-#define SPC_R(MT) hipLaunchKernelGGL((k_linear_rows<T, MT, 8>), grid, dim3(512), 0, s, a)
-    if (a.m <= 16) SPC_R(1);
-    else if (a.m <= 32) SPC_R(2);
-    else SPC_R(4);
-#undef SPC_R
+#define SPC_R(MT, NT, WAVES)                                                                                          \
+  hipLaunchKernelGGL((k_linear_rows<T, MT, NT, WAVES>),                                                               \
+                     dim3((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)((a.m + 16 * MT - 1) / (16 * MT))), \
+                     dim3(64 * WAVES), 0, s, a)
+// a wave for each block of columns, up to WAVES
+#define SPC_W(MT, NT, WAVES)              \
+  do {                                    \
+    if (a.kb <= 4) SPC_R(MT, NT, 4);      \
+    else if (a.kb <= 8) SPC_R(MT, NT, 8); \
+    else SPC_R(MT, NT, WAVES);            \
+  } while (0)
+  if (few_rows(a)) {
+    if (a.m <= 16) SPC_W(1, 1, 16);
+    else if (a.m <= 32) SPC_W(2, 1, 16);
+    else if (a.m <= 48) SPC_W(3, 1, 16);
+    else if (a.m <= 64) SPC_W(4, 1, 16);
+    else SPC_R(4, 2, 8);
     return;
   }
+#undef SPC_W
+#undef SPC_R
 #define SPC_T(EXACT, BM, BN, WM, WN)                                                                                  \
   hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN>),                                                       \
                      dim3((unsigned)(((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN))), dim3(64 * WM * WN), 0, s, a)
