@@ -8,6 +8,7 @@ raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 
 import torch
@@ -251,13 +252,6 @@ def spconv_concat_rows(a: torch.Tensor, b: torch.Tensor, out: torch.Tensor | Non
     return out
 
 
-def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, n: int, c: int) -> None:
-    """Rows [n][c] with columns that follow each other."""
-    if t.dtype is not dtype or t.shape != (n, c) or (c > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected rows {(n, c)} of {dtype}, got {t.dtype} {tuple(t.shape)} with strides "
-                         f"{t.stride()}")
-
-
 def _ld(t: torch.Tensor) -> int:
     """Row stride; that of a single row is its length (torch's may be anything)."""
     n, c = t.shape
@@ -474,12 +468,23 @@ SCALE_BLOCK = 128  # columns of an 8-bit row (and rows of 8-bit weights) that sh
 E4M3 = torch.float8_e4m3fn
 
 
-def _empty(shape, dtype, like: torch.Tensor, stream=None) -> torch.Tensor:
-    """Device memory that belongs to the stream which the call runs on."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+_ops = None
+
+
+def _load_ops():
+    """The operators' binding (csrc/torch_ops.cpp), bound to the library."""
+    global _ops
+    if _ops is None:
+        path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_torch_ops.so")
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is not built; run __graft_entry__.build() (no fallback exists)")
+        spec = importlib.util.spec_from_file_location("paper_2401_06145_amd._torch_ops", path)
+        ops = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(ops)
+        ops.bind(*(ctypes.cast(getattr(lib(), f), ctypes.c_void_p).value for f in (
+            "spconv_rms_norm", "spconv_scaled_linear", "spconv_attention", "spconv_attention_workspace_bytes")), _check)
+        _ops = ops
+    return _ops
 
 
 def rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
@@ -488,39 +493,20 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: torch.Tensor | None
 
     y is in x's type and scale None, or with ``bits8`` y is e4m3 and scale float32 [n][ceil(c / 128)];
     sum is x + residual in x's type (None without a residual)."""
-    n, c = x.shape
-    dtype = x.dtype
-    if dtype not in DTYPES:
-        raise ValueError(f"x: {dtype} is not one of the layers' types")
-    _rows("x", x, dtype, n, c)
-    if gamma.dtype is not dtype or gamma.shape != (c,) or not gamma.is_contiguous():
-        raise ValueError(f"gamma: expected contiguous {dtype} {(c,)}, got {gamma.dtype} {tuple(gamma.shape)}")
-    total = scale = None
-    if residual is not None:
-        _rows("residual", residual, dtype, n, c)
-        total = _empty((n, c), dtype, x, stream)
-    y = _empty((n, c), E4M3 if bits8 else dtype, x, stream)
-    if bits8:
-        scale = _empty((n, -(-c // SCALE_BLOCK)), torch.float32, x, stream)
-    spconv_rms_norm(x, residual, gamma, total, y, scale, eps, stream)
-    return y, scale, total
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm(x, gamma, residual, eps, bits8)
+    return (_ops or _load_ops()).rms_norm(x, gamma, residual, eps, bits8)
 
 
 def scaled_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, dtype: torch.dtype,
                   relu: bool = False, exact: bool = False, stream=None) -> torch.Tensor:
     """Product of e4m3 rows x [m][k] and e4m3 weights w [n][k] with their scales, in ``dtype``.
     ``exact``: every sum in float32 also in 16-bit types (slower; spconv_scaled_linear in spconv.h)."""
-    m, k = x.shape
-    n, kb = w.shape[0], -(-k // SCALE_BLOCK)
-    _rows("x", x, E4M3, m, k)
-    _rows("w", w, E4M3, n, k)
-    _rows("x_scale", x_scale, torch.float32, m, kb)
-    _rows("w_scale", w_scale, torch.float32, -(-n // SCALE_BLOCK), kb)
-    if dtype not in DTYPES:
-        raise ValueError(f"{dtype} is not one of the layers' types")
-    y = _empty((m, n), dtype, x, stream)
-    spconv_scaled_linear(x, x_scale, w, w_scale, y, relu, exact, stream)
-    return y
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return scaled_linear(x, x_scale, w, w_scale, dtype, relu, exact)
+    return (_ops or _load_ops()).scaled_linear(x, x_scale, w, w_scale, dtype, relu, exact)
 
 
 def quantize_weight(w: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
@@ -536,19 +522,6 @@ def quantize_weight(w: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
     return q.clamp(-448.0, 448.0).to(E4M3), scale
 
 
-def _heads(name: str, t: torch.Tensor, dtype: torch.dtype, head_dim: int) -> None:
-    if t.dim() != 3 or t.dtype is not dtype or t.shape[2] != head_dim or t.stride(2) != 1:
-        raise ValueError(f"{name}: expected [rows][heads][{head_dim}] of {dtype}, got {t.dtype} {tuple(t.shape)} with "
-                         f"strides {t.stride()}")
-
-
-def _int32(name: str, t: torch.Tensor, shape) -> int:
-    """The address of a contiguous int32 array."""
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected contiguous int32 {shape}, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr()
-
-
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, k_start: torch.Tensor,
               max_q: int, max_k: int, k_len: torch.Tensor | None = None, prefix: torch.Tensor | None = None,
               causal: bool = False, scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
@@ -558,30 +531,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.
     q [n_q][heads][d], k and v [n_k][kv_heads][d] may be slices of a fused product; q_start and
     k_start int32 [docs + 1]; k_len int32 [docs] where k and v are caches; scale defaults to
     1 / sqrt(d).  Returns [n_q][heads][d]."""
-    n_q, heads, d = q.shape
-    n_k, kv_heads = k.shape[0], k.shape[1]
-    dtype = q.dtype
-    if dtype not in DTYPES:
-        raise ValueError(f"q: {dtype} is not one of the layers' types")
-    _heads("q", q, dtype, d)
-    _heads("k", k, dtype, d)
-    _heads("v", v, dtype, d)
-    if v.shape != k.shape:
-        raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
-    docs = q_start.shape[0] - 1
-    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.shape != (heads,)
-                               or not slopes.is_contiguous()):
-        raise ValueError(f"slopes: expected contiguous float32 {(heads,)}, got {slopes.dtype} {tuple(slopes.shape)}")
-    out = _empty((n_q, heads, d), dtype, q, stream)
-    a = AttentionArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *q.stride()[:2], *k.stride()[:2],
-                      *v.stride()[:2], heads * d, d, _int32("q_start", q_start, (docs + 1,)),
-                      _int32("k_start", k_start, (docs + 1,)), None if k_len is None else _int32("k_len", k_len, (docs,)),
-                      None if prefix is None else _int32("prefix", prefix, (docs,)),
-                      None if slopes is None else slopes.data_ptr(),
-                      None if q_pos is None else _int32("q_pos", q_pos, (n_q, 4)),
-                      None if k_pos is None else _int32("k_pos", k_pos, (n_k, 4)), n_q, n_k, docs, max_q, max_k, heads,
-                      kv_heads, d, DTYPES[dtype], causal, d ** -0.5 if scale is None else scale, cap)
-    need = spconv_attention_workspace_bytes(a)
-    workspace = _empty(need, torch.uint8, q, stream) if need else None
-    spconv_attention(a, workspace, _device_stream(q, stream))
-    return out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attention(q, k, v, q_start, k_start, max_q, max_k, k_len, prefix, causal, scale, cap, slopes, q_pos, k_pos)
+    return (_ops or _load_ops()).attention(q, k, v, q_start, k_start, max_q, max_k, k_len, prefix, causal, scale, cap,
+                                           slopes, q_pos, k_pos)
