@@ -23,30 +23,55 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
   const int lane = threadIdx.x % kWave;
   if (at >= rows) return;
-  float top = a.floor;
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x2 ml = a.part_ml[(int64_t)s * rows + at];
-    top = fmaxf(top, ml[0]);
-  }
-  float sum = 0.0f;
-  f32x4 v = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x2 ml = a.part_ml[(int64_t)s * rows + at];
-    if (ml[1] == 0.0f) continue;
-    const float by = __builtin_amdgcn_exp2f((ml[0] - top) * a.exp_by);
-    sum = fmaf(ml[1], by, sum);
-    if (4 * lane < a.d) {
-      const f32x4 p = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)s * rows + at) * a.d + 4 * lane);
+  // the ranges' maxima and sums, one a lane
+  float top = a.floor, sum = 0.0f;
+  for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + at][0]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = fmaf(p[i], by, v[i]);
+  for (int i = 1; i < kWave; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+  // their outputs: a group of lanes a range, four columns a lane
+  const int wide = (a.d + 3) / 4 <= 8 ? 8 : (a.d + 3) / 4 <= 16 ? 16 : (a.d + 3) / 4 <= 32 ? 32 : 64;
+  const int x = 4 * (lane % wide), groups = kWave / wide;
+  f32x4 v = {0, 0, 0, 0};
+  for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+    const int s = s0 + lane;
+    float by = 0.0f;
+    if (s < a.splits) {
+      const f32x2 ml = a.part_ml[(int64_t)s * rows + at];
+      if (ml[1] != 0.0f) {  // a range without keys has written nothing else
+        by = __builtin_amdgcn_exp2f((ml[0] - top) * a.exp_by);
+        sum = fmaf(ml[1], by, sum);
+      }
+    }
+    const int here = std::min(a.splits - s0, kWave);
+    for (int i0 = 0; i0 < here; i0 += 4 * groups) {  // all lanes take part in the exchange
+      f32x4 p[4];
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * groups + lane / wide;
+        const float from = __shfl(by, i);
+        w[u] = i < here ? from : 0.0f;
+        p[u] = f32x4{0, 0, 0, 0};
+        if (w[u] != 0.0f && x < a.d)
+          p[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + i) * rows + at) * a.d + x);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(p[u][j], w[u], v[j]);
     }
   }
-  if (4 * lane >= a.d) return;
+#pragma unroll
+  for (int i = 1; i < kWave; i *= 2) sum += __shfl_xor(sum, i);
+  for (int i = wide; i < kWave; i *= 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], i);
+  if (lane >= wide || x >= a.d) return;
   const float inv = 1.0f / sum;
   float r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = sum == 0.0f ? 0.0f : v[i] * inv;
-  store4(static_cast<T*>(a.out) + at / a.heads * a.out_row + at % a.heads * a.out_head + 4 * lane, r);
+  store4(static_cast<T*>(a.out) + at / a.heads * a.out_row + at % a.heads * a.out_head + x, r);
 }
 
 template <typename T>
@@ -65,10 +90,13 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
   if (p.rows && n_docs > 65535) p.rows = false;
   p.slots = n_q / kQueryTile + n_docs;
   const int64_t work = p.rows ? (int64_t)n_docs * kv_heads : (n_q / kQueryTile + std::min<int64_t>(n_docs, n_q)) * heads;
-  // key ranges until a launch has about four workgroups per CU, of at least 128 keys
-  int splits = 1;
-  while (splits < 64 && work * splits < 1024 && max_k / (2 * splits) >= 128) splits *= 2;
-  p.chunk = std::max(128, (int)(((int64_t)max_k + splits - 1) / splits + 127) / 128 * 128);
+  // Ranges of keys until a launch has about 4096 workgroups of the few-query form (documents
+  // differ in length: 48 caches of up to 8192 keys take 186 us with 1024, 176 with 2048, 163 with 4096
+  // and, as a workgroup has to pay for its start, 231 with 6144), about 2048 of the other (voxels of two
+  // frames, three ranges: 206 us; two: 214, four: 224), of 256 keys at least (one document of
+  // 16,000 keys: 30 us, and 45 with ranges of 128, whose results take longer to join).
+  const int64_t chunk = ((int64_t)max_k * work / (p.rows ? 4096 : 2048) + 127) / 128 * 128;
+  p.chunk = (int)std::min<int64_t>(std::max<int64_t>(chunk, 256), 0x7fffff80);
   p.splits = std::max(1, (max_k + p.chunk - 1) / p.chunk);
   return p;
 }

@@ -11,12 +11,16 @@ using namespace attn;
 // at a time, each on its own, and join their results through LDS at the end.  K comes from
 // memory straight into registers, V through a strip of LDS that only its wave uses.
 // ---------------------------------------------------------------------------
+//
+// What bounds it: memory.  48 caches of up to 8192 keys (8 key heads of 128, 16 bits, 798 MB) take
+// 156 us, 5.1 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
+// way (one: 183 us), except for rows of more than 256 bytes, whose registers would spill.
 template <typename T, int D, int NC>
-__global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
+__global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
   constexpr int E = sizeof(T), ROW = D * E, KT = 32;
   typedef Lds<ROW> L;
-  constexpr int P = KT * L::CH / kWave;
+  constexpr int P = KT * (int)L::CH / kWave;
   constexpr int STRIP = KT * ROW > D * 16 * 4 ? KT * ROW : D * 16 * 4;
   __shared__ __align__(16) char strips[4][STRIP];
   __shared__ f32x4 spos[4][KT];
@@ -59,9 +63,13 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
   const T* kp = static_cast<const T*>(a.k) + d.k0 * a.k_row + (int64_t)kvh * a.k_head;
   const T* vp = static_cast<const T*>(a.v) + d.k0 * a.v_row + (int64_t)kvh * a.v_head;
 
-  for (int k0 = k_begin + wave * KT; k0 < k_end; k0 += 4 * KT) {
-    const bool masked = k0 + KT > lim_lo;
-    Frag fk[2][D / 32];
+  // A tile's operands: K's rows as the product takes them, V's as they lie, the voxels of the
+  // first KT lanes.  Their registers take the next tile as soon as they are used, so that its
+  // loads are under way for the rest of the work on this one.
+  Frag fk[2][D / 32];
+  u32x4 rv[P];
+  f32x4 pos = {0, 0, 0, 0};
+  const auto fetch_k = [&](int k0) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int key = k0 + 16 * h + c16;
@@ -72,44 +80,63 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
         fk[h][k] = key < d.len_k && at < a.d ? load_frag(p + at) : zero_frag<T>();
       }
     }
-    bool bad = false;
-    u32x4 rv[P];
+  };
+  const auto fetch_v = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int p = lane + kWave * i, r = p / L::CH, c = p % L::CH;
+      const int p = lane + kWave * i, r = p / (int)L::CH, c = p % (int)L::CH;
       rv[i] = u32x4{0, 0, 0, 0};
       if (k0 + r < d.len_k && c * (16 / E) < a.d)
         rv[i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
-      if (masked) bad |= odd_values<T>(rv[i]);
     }
     if (a.k_pos && lane < KT) {
-      f32x4 pos = {0, 0, 0, 0};
+      pos = f32x4{0, 0, 0, 0};
       if (k0 + lane < d.len_k) {
         const int32_t* p = a.k_pos + 4 * (d.k0 + k0 + lane);
         pos = f32x4{(float)p[1], (float)p[2], (float)p[3], 0};
       }
-      spos[wave][lane] = pos;
     }
+  };
+  const int k_first = k_begin + wave * KT;
+  if (k_first < k_end) {
+    fetch_v(k_first);
+    fetch_k(k_first);
+  }
+  for (int k0 = k_first; k0 < k_end; k0 += 4 * KT) {
+    const bool masked = k0 + KT > lim_lo;
+    bool bad = false;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) bad |= odd_values<T>(rv[i]);
+    }
+    if (a.k_pos && lane < KT) spos[wave][lane] = pos;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int p = lane + kWave * i, r = p / L::CH, c = p % L::CH;
+      const int p = lane + kWave * i, r = p / (int)L::CH, c = p % (int)L::CH;
       *reinterpret_cast<u32x4*>(sv + r * ROW + 16 * L::v_chunk16(r, c)) = rv[i];
     }
+    const bool more = k0 + 4 * KT < k_end;
+    if (more) fetch_v(k0 + 4 * KT);
     const bool careful = masked && __any(bad);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
+    f32x4 s[NC][2];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[n][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) s[n][h] = Mat<T>::mma16(fk[h][k], fq[n][k], s[n][h]);
+      }
+    if (more) fetch_k(k0 + 4 * KT);
     Frag fp[NC];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) s[h] = Mat<T>::mma16(fk[h][k], fq[n][k], s[h]);
       float sc[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sc[i] = s[i / 4][i % 4];
+      for (int i = 0; i < 8; ++i) sc[i] = s[n][i / 4][i % 4];
       const auto at = [&](int i) { return 16 * (i / 4) + 4 * g + i % 4; };
       to_scores<8>(a, q[n], sc, masked, [&](int i) { return k0 + at(i); }, [&](int i) { return spos[wave][at(i)]; });
       float top = m[n];
