@@ -318,7 +318,8 @@ int spconv_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64
  * 128 products are summed by the 8-bit matrix instruction, which drops a product 2^13 times
  * smaller than the largest of its group of eight, unless exact != 0: then, as for SPCONV_F32
  * and few rows always, they are summed in float32, at about half the speed.  k, ld_x and ld_w multiples of 16 (16-byte rows;
- * SPCONV_EUNSUPPORTED otherwise), d_x and d_w 16-byte aligned; any m and n.  k = 0 gives zeros.
+ * SPCONV_EUNSUPPORTED otherwise), rows of d_x, d_w and d_x_scale at most 8 MiB apart, d_x and d_w
+ * 16-byte aligned; any m and n.  k = 0 gives zeros.
  * d_y must not overlap the inputs. */
 int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, int64_t ld_x_scale,
                          const void* d_w, int64_t ld_w, const float* d_w_scale, int64_t ld_w_scale, void* d_y,
@@ -341,7 +342,8 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
  *               a fused product will do); head_dim elements follow each other.
  *   max_q, max_k  at least the longest document's queries and keys: keys behind are not read,
  *               queries behind get no output.
- * head_dim a multiple of 8 up to 256, 16-byte aligned pointers.  d_q_start must not descend.
+ * head_dim a multiple of 8 up to 256, 16-byte aligned pointers, rows of d_k and d_v at most
+ * 32 MiB apart, max_k at most 2^30.  d_q_start must not descend.
  * Softmax statistics and sums are float32; the exponentials are rounded to `dtype` for the
  * product with V. */
 typedef struct {

@@ -1110,6 +1110,7 @@ int check_attention(const spconv_attention_args* a) {
   if (a->n_q > 0x7fffffff || a->n_k > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
   if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads != 0)
     return fail(SPCONV_EINVAL, "heads must be a multiple of kv_heads");
+  if (a->max_k > 1 << 30) return fail(SPCONV_EUNSUPPORTED, "more than 2^30 keys in a document");
   if (a->heads > 65535) return fail(SPCONV_EUNSUPPORTED, "more than 65535 heads");
   if (a->head_dim < 8 || a->head_dim > 256 || a->head_dim % 8 != 0)
     return fail(SPCONV_EUNSUPPORTED, "head_dim must be a multiple of 8 up to 256");

@@ -90,13 +90,13 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
   if (p.rows && n_docs > 65535) p.rows = false;
   p.slots = n_q / kQueryTile + n_docs;
   const int64_t work = p.rows ? (int64_t)n_docs * kv_heads : (n_q / kQueryTile + std::min<int64_t>(n_docs, n_q)) * heads;
-  // Ranges of keys until a launch has about 4096 workgroups of the few-query form (documents
-  // differ in length: 48 caches of up to 8192 keys take 186 us with 1024, 176 with 2048, 163 with 4096
-  // and, as a workgroup has to pay for its start, 231 with 6144), about 2048 of the other (voxels of two
-  // frames, three ranges: 206 us; two: 214, four: 224), of 256 keys at least (one document of
-  // 16,000 keys: 30 us, and 45 with ranges of 128, whose results take longer to join).
-  const int64_t chunk = ((int64_t)max_k * work / (p.rows ? 4096 : 2048) + 127) / 128 * 128;
-  p.chunk = (int)std::min<int64_t>(std::max<int64_t>(chunk, 256), 0x7fffff80);
+  // Ranges of equal length: until a launch has about 3072 workgroups of the few-query form (48
+  // caches of up to 8192 keys, 8 key heads: 209 us with one range, 168 to 160 with 5 to 16, 178 with 22), or about
+  // 2048 of the other (voxels of two frames, 696 workgroups a range: 217 us with one or two,
+  // 199 with three, 209 with six), but of 256 keys at least (a document of 16,000 keys 24 us).
+  int64_t splits = ((p.rows ? 3072 : 2048) + work - 1) / std::max<int64_t>(work, 1);
+  splits = std::max<int64_t>(1, std::min<int64_t>(splits, max_k / 256));
+  p.chunk = (int)std::max<int64_t>(128, (((int64_t)max_k + splits - 1) / splits + 127) / 128 * 128);
   p.splits = std::max(1, (max_k + p.chunk - 1) / p.chunk);
   return p;
 }

@@ -171,10 +171,9 @@ __device__ __forceinline__ int find_doc(const AttnArgs& a, int slot, int tile, i
   return lo;
 }
 
-// Turns products q.k of one query into the scores that the running maximum is taken of;
-// key(i) is the document's key of product i.  Capped scores are in units of log2; the others
-// stay in those of the bare products (exp_by folds their scale into the exponential's).
-// Hidden keys get -inf.
+// Scores of one query, as the running maximum is taken of them: capped ones are in units of
+// log2, the others in those of the products q.k (exp_by folds their scale into the
+// exponential's).  key(i) is the document's key of product i; hidden keys get -inf.
 struct Query {
   float place, slope;  // place among the keys; slope in the scores' units
   float x, y, z;       // voxel
@@ -207,37 +206,45 @@ __device__ __forceinline__ void cap_scores(const AttnArgs& a, float* s) {
   }
 }
 
-template <int COUNT, typename Key, typename Pos>
-__device__ __forceinline__ void to_scores(const AttnArgs& a, const Query& q, float* s, bool masked, Key key, Pos pos) {
-  if (a.cap > 0.0f) cap_scores<COUNT>(a, s);
-  if (a.slopes) {
-    if (a.k_pos) {
-#pragma unroll
-      for (int i = 0; i < COUNT; ++i) {
-        const f32x4 p = pos(i);
-        const float dx = p[0] - q.x, dy = p[1] - q.y, dz = p[2] - q.z;
-        s[i] = fmaf(-q.slope, __builtin_amdgcn_sqrtf(fmaf(dx, dx, fmaf(dy, dy, dz * dz))), s[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < COUNT; ++i) s[i] = fmaf(-q.slope, fabsf(q.place - (float)key(i)), s[i]);
-    }
-  }
-  if (masked) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) s[i] = key(i) < q.lim ? s[i] : -INFINITY;
-  }
+// A voxel from its row (b, x, y, z), seen from `origin` (another such row): small numbers,
+// exact in float32, wherever the scene lies.
+struct Voxel {
+  float x, y, z;
+};
+__device__ __forceinline__ Voxel voxel_from(const int32_t* p, const int32_t* origin) {
+  return Voxel{(float)((int64_t)p[1] - origin[1]), (float)((int64_t)p[2] - origin[2]), (float)((int64_t)p[3] - origin[3])};
 }
 
-__device__ __forceinline__ Query make_query(const AttnArgs& a, const Doc& d, int i, int head) {
+template <int COUNT, typename Pos>
+__device__ __forceinline__ void add_voxel_bias(const Query& q, float* s, Pos pos) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) {
+    const Voxel p = pos(i);
+    const float dx = p.x - q.x, dy = p.y - q.y, dz = p.z - q.z;
+    s[i] = fmaf(-q.slope, __builtin_amdgcn_sqrtf(fmaf(dx, dx, fmaf(dy, dy, dz * dz))), s[i]);
+  }
+}
+template <int COUNT, typename Key>
+__device__ __forceinline__ void add_place_bias(const Query& q, float* s, Key key) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) s[i] = fmaf(-q.slope, fabsf(q.place - (float)key(i)), s[i]);
+}
+template <int COUNT, typename Key>
+__device__ __forceinline__ void hide(const Query& q, float* s, Key key) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) s[i] = key(i) < q.lim ? s[i] : -INFINITY;
+}
+
+// `origin`: the row that voxels are seen from, or NULL where there are none.
+__device__ __forceinline__ Query make_query(const AttnArgs& a, const Doc& d, int i, int head, const int32_t* origin) {
   Query q;
   q.lim = seen(a, d, i);
   q.place = (float)(d.len_k - d.len_q + i);
   q.slope = a.slopes ? a.slopes[head] * a.slope_by : 0.0f;
   q.x = q.y = q.z = 0.0f;
-  if (a.q_pos) {
-    const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + i);
-    q.x = (float)p[1], q.y = (float)p[2], q.z = (float)p[3];
+  if (origin) {
+    const Voxel v = voxel_from(a.q_pos + 4 * (int64_t)(d.q0 + i), origin);
+    q.x = v.x, q.y = v.y, q.z = v.z;
   }
   return q;
 }

@@ -12,8 +12,8 @@ using namespace attn;
 // memory straight into registers, V through a strip of LDS that only its wave uses.
 // ---------------------------------------------------------------------------
 //
-// What bounds it: memory.  48 caches of up to 8192 keys (8 key heads of 128, 16 bits, 798 MB) take
-// 156 us, 5.1 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
+// What bounds it: memory.  48 caches of up to 8192 keys (8 key heads of 128, 16 bits, 801 MB) take
+// 156 to 160 us, 5.0 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
 // way (one: 183 us), except for rows of more than 256 bytes, whose registers would spill.
 template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void k_attn_rows(AttnArgs a) {
@@ -26,13 +26,17 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   __shared__ f32x4 spos[4][KT];
   __shared__ float sm[4][16 * NC], sl[4][16 * NC];
 
+  // Workgroups go around the 8 XCDs: each document and head begins with another range, or some
+  // XCDs would get the ranges that only long documents fill (8 ranges of 48 caches: 219 us, so 160).
   const int doc = blockIdx.z, kvh = blockIdx.y;
+  const int split = (blockIdx.x + doc + kvh) % a.splits;
   const Doc d = load_doc(a, doc);
   const int group = a.heads / a.kv_heads, cols = d.len_q * group;
   if (cols <= 0) return;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, c16 = lane % 16, g = lane / 16;
   char* sv = strips[wave];
 
+  const int32_t* origin = a.q_pos ? a.q_pos + 4 * (int64_t)d.q0 : nullptr;
   Query q[NC];
   Frag fq[NC][D / 32];
   int64_t row[NC];  // row of the packed queries times heads, plus the head
@@ -40,7 +44,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   for (int n = 0; n < NC; ++n) {
     const int col = std::min(16 * n + c16, cols - 1), i = col / group, head = kvh * group + col % group;
     row[n] = (int64_t)(d.q0 + i) * a.heads + head;
-    q[n] = make_query(a, d, i, head);
+    q[n] = make_query(a, d, i, head, origin);
     const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + i) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {
@@ -49,7 +53,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
   }
   const int lim_lo = seen(a, d, 0), lim_hi = seen(a, d, d.len_q - 1);
-  const int k_begin = blockIdx.x * a.chunk, k_end = std::min(lim_hi, k_begin + a.chunk);
+  const int k_begin = split * a.chunk, k_end = std::min(lim_hi, k_begin + a.chunk);
 
   f32x4 o[NC][D / 16];
   float m[NC], l[NC];
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   // loads are under way for the rest of the work on this one.
   Frag fk[2][D / 32];
   u32x4 rv[P];
-  f32x4 pos = {0, 0, 0, 0};
+  Voxel pos = {0, 0, 0};
   const auto fetch_k = [&](int k0) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -90,11 +94,8 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         rv[i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
     }
     if (a.k_pos && lane < KT) {
-      pos = f32x4{0, 0, 0, 0};
-      if (k0 + lane < d.len_k) {
-        const int32_t* p = a.k_pos + 4 * (d.k0 + k0 + lane);
-        pos = f32x4{(float)p[1], (float)p[2], (float)p[3], 0};
-      }
+      pos = Voxel{0, 0, 0};
+      if (k0 + lane < d.len_k) pos = voxel_from(a.k_pos + 4 * (d.k0 + k0 + lane), origin);
     }
   };
   const int k_first = k_begin + wave * KT;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
       for (int i = 0; i < P; ++i) bad |= odd_values<T>(rv[i]);
     }
-    if (a.k_pos && lane < KT) spos[wave][lane] = pos;
+    if (a.k_pos && lane < KT) spos[wave][lane] = f32x4{pos.x, pos.y, pos.z, 0};
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int p = lane + kWave * i, r = p / (int)L::CH, c = p % (int)L::CH;
@@ -138,7 +139,17 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
       for (int i = 0; i < 8; ++i) sc[i] = s[n][i / 4][i % 4];
       const auto at = [&](int i) { return 16 * (i / 4) + 4 * g + i % 4; };
-      to_scores<8>(a, q[n], sc, masked, [&](int i) { return k0 + at(i); }, [&](int i) { return spos[wave][at(i)]; });
+      const auto key = [&](int i) { return k0 + at(i); };
+      if (a.cap > 0.0f) cap_scores<8>(a, sc);
+      if (a.k_pos) {
+        add_voxel_bias<8>(q[n], sc, [&](int i) {
+          const f32x4 p = spos[wave][at(i)];
+          return Voxel{p[0], p[1], p[2]};
+        });
+      } else if (a.slopes) {
+        add_place_bias<8>(q[n], sc, key);
+      }
+      if (masked) hide<8>(q[n], sc, key);
       float top = m[n];
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, sc[i]);
@@ -240,7 +251,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
     __syncthreads();
     if (16 * n + c16 < cols) {
-      const int64_t part = (int64_t)blockIdx.x * a.n_q * a.heads + row[n];
+      const int64_t part = (int64_t)split * a.n_q * a.heads + row[n];
       if (a.splits > 1 && wave == 0 && g == 0) a.part_ml[part] = f32x2{top, sum};
       const float inv = 1.0f / sum;
       for (int t = wave; t < D / 16; t += 4) {

@@ -7,8 +7,9 @@ using namespace attn;
 
 // What the scores go through.  kBare: nothing but their scale.  kCapped: a cap of at most 60
 // and no bias, in types of float32's exponent range: exp(score) itself lies between e^-60 and
-// e^60, so there is no running maximum to keep.  kAny: everything else.
-enum Mode { kBare, kCapped, kAny };
+// e^60, so there is no running maximum to keep.  kVoxel: a bias by the distance of voxels, with
+// or without a cap.  kAny: everything else.
+enum Mode { kBare, kCapped, kVoxel, kAny };
 constexpr float kCapWithoutMaximum = 60.0f;
 
 // 16 bytes a lane from memory straight into LDS, P times: those at `at[i]` of the `bytes` that
@@ -38,7 +39,31 @@ __device__ __forceinline__ void bring_rows(const char* from, int bytes, char* to
 }
 
 // Workgroups a CU holds, by the registers that rows of this many bytes need.
-constexpr int waves_a_simd(int row) { return row <= 64 ? 4 : row <= 128 ? 3 : row <= 256 ? 2 : 1; }
+constexpr int waves_a_simd(int row, int mode) {
+  return row <= 64 ? (mode == kVoxel ? 3 : 4) : row <= 128 ? (mode == kVoxel ? 2 : 3) : row <= 256 ? 2 : 1;
+}
+
+// Distances of voxels by the matrix unit: |k - q|^2 = |q|^2 - 2 k.q + |k|^2 is a product of five
+// columns, float32, two instructions for 32 x 32 distances instead of six a distance (voxels of two
+// frames 214 -> 199 us).  It must not lose small distances in the difference of large
+// squares: it is taken where every sum is a whole number of float32, that is where the voxels
+// of a tile, as multiples of 2^shift that the queries have in common, are at most 1182 apart
+// from the origin in each axis (3 1182^2 < 2^22, and four such squares still fit 2^24).
+constexpr int kVoxelReach = 1182;
+struct Near {
+  int shift;
+  __device__ bool operator()(const int32_t* p, const int32_t* origin) const {
+    uint32_t all = 0;
+    int64_t most = 0;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      const int64_t v = (int64_t)p[i] - origin[i];
+      all |= (uint32_t)v;
+      most = std::max(most, v < 0 ? -v : v);
+    }
+    return (all & ((1u << shift) - 1)) == 0 && most <= (int64_t)kVoxelReach << shift;
+  }
+};
 
 // A workgroup of four waves takes 128 queries of one head and one range of keys, KT keys at a
 // time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
@@ -48,7 +73,7 @@ constexpr int waves_a_simd(int row) { return row <= 64 ? 4 : row <= 128 ? 3 : ro
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
 // where the call is causal) start first.
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T), MODE)) void k_attn_tile(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
   constexpr int QT = kQueryTile, E = sizeof(T), ROW = D * E;
   constexpr int KT = ROW >= 1024 ? 32 : 64;
@@ -56,12 +81,13 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
   // the first product, a strip of V while the exponentials are computed (784 -> 770 us on whole
   // documents of 128 columns; with distances, or 2 strips, the registers spill; shorter
   // rows gain nothing).
-  constexpr bool AHEAD = ROW == 256 && MODE != kAny;
+  constexpr bool AHEAD = ROW == 256 && MODE < kVoxel;
   constexpr int VA = AHEAD ? 1 : 0;
   typedef Lds<ROW> L;
   constexpr int P = KT * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
   __shared__ __align__(16) char sk[2][KT * ROW], sv[2][KT * ROW];
-  __shared__ f32x4 spos[2][KT];
+  __shared__ f32x4 spos[2][KT];       // voxels of the keys: x, z, y, x^2 + y^2 + z^2
+  __shared__ uint32_t snear[2], sbits;  // whether they all are near; bits of the queries' voxels
   __shared__ uint32_t odd_at[3 * KT * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
 
   // which slot, head and range of keys
@@ -79,7 +105,8 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
 
   // the rows of this wave, and what they see
   const int row = i0 + wave * 32 + c32;
-  const Query q = make_query(a, d, std::min(row, d.len_q - 1), head);
+  const int32_t* origin = MODE == kVoxel ? a.q_pos + 4 * (int64_t)(d.q0 + i0) : nullptr;
+  const Query q = make_query(a, d, std::min(row, d.len_q - 1), head, origin);
   Frag fq[D / 16];
   {
     const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + std::min(row, d.len_q - 1)) * a.q_row + (int64_t)head * a.q_head;
@@ -120,18 +147,46 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
     bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
     bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
   };
-  const auto voxel = [&](int k0) {
-    f32x4 p = {0, 0, 0, 0};
-    if (MODE == kAny && a.k_pos && threadIdx.x < KT && k0 + (int)threadIdx.x < d.len_k) {
-      const int32_t* v = a.k_pos + 4 * (d.k0 + k0 + threadIdx.x);
-      p = f32x4{(float)v[1], (float)v[2], (float)v[3], 0};
+  // the first KT threads, one wave: a key's voxel each
+  Near near = {0};
+  bool near_q = false;
+  if constexpr (MODE == kVoxel) {
+    const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + std::min(row, d.len_q - 1));
+    if (threadIdx.x == 0) sbits = 0;
+    __syncthreads();
+    atomicOr(&sbits, ((uint32_t)p[1] - (uint32_t)origin[1]) | ((uint32_t)p[2] - (uint32_t)origin[2]) |
+                         ((uint32_t)p[3] - (uint32_t)origin[3]));
+    __syncthreads();
+    near.shift = __builtin_ctz(sbits | 1u << 4);  // 16 is the spacing of the coarsest level
+    near_q = __all(near(p, origin));
+  }
+  f32x4 voxel;
+  bool voxel_near;
+  const auto fetch_voxel = [&](int k0) {
+    voxel = f32x4{0, 0, 0, 0};
+    voxel_near = true;
+    if (MODE == kVoxel && threadIdx.x < KT && k0 + (int)threadIdx.x < d.len_k) {
+      const int32_t* p = a.k_pos + 4 * (d.k0 + k0 + threadIdx.x);
+      const Voxel v = voxel_from(p, origin);
+      voxel = f32x4{v.x, v.z, v.y, fmaf(v.x, v.x, fmaf(v.y, v.y, v.z * v.z))};
+      voxel_near = near(p, origin);
     }
-    return p;
   };
+  const auto keep_voxel = [&](int b) {
+    if (MODE == kVoxel && wave == 0) {
+      if (lane < KT) spos[b][lane] = voxel;
+      const bool all = __all(voxel_near);
+      if (lane == 0) snear[b] = all;
+    }
+  };
+  // this lane's part of the second operand of the distances, and |q|^2
+  const float vq0 = -2.0f * (half ? q.y : q.x), vq1 = half ? 1.0f : -2.0f * q.z;
+  const float vq2 = fmaf(q.x, q.x, fmaf(q.y, q.y, q.z * q.z));
 
   if (k_begin < k_end) {
     bring(k_begin, 0);
-    if (MODE == kAny && a.k_pos && threadIdx.x < KT) spos[0][threadIdx.x] = voxel(k_begin);
+    fetch_voxel(k_begin);
+    keep_voxel(0);
   }
   int b = 0;
   for (int k0 = k_begin; k0 < k_end; k0 += KT, b ^= 1) {
@@ -162,10 +217,9 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
         __syncthreads();
       }
     }
-    f32x4 next_voxel;
     if (k0 + KT < k_end) {
       bring(k0 + KT, b ^ 1);
-      if (MODE == kAny) next_voxel = voxel(k0 + KT);
+      fetch_voxel(k0 + KT);
     }
     if (k0 < lim_hi) {  // else nothing for this wave
       float s[KT / 2];
@@ -247,12 +301,31 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
           for (int i = 0; i < KT / 2; ++i) s[i] = k0 + at(i) < q.lim ? s[i] : 0.0f;
         }
       } else {
-        if constexpr (MODE == kAny) {
-          to_scores<KT / 2>(a, q, s, masked, [&](int i) { return k0 + at(i); }, [&](int i) { return spos[b][at(i)]; });
-        } else if (masked) {
+        const auto key = [&](int i) { return k0 + at(i); };
+        if (MODE != kBare && a.cap > 0.0f) cap_scores<KT / 2>(a, s);
+        if constexpr (MODE == kVoxel) {
+          if (near_q && snear[b]) {
 #pragma unroll
-          for (int i = 0; i < KT / 2; ++i) s[i] = k0 + at(i) < q.lim ? s[i] : -INFINITY;
+            for (int h = 0; h < KT / 32; ++h) {
+              const f32x2 k = *reinterpret_cast<const f32x2*>(reinterpret_cast<const char*>(&spos[b][32 * h + c32]) + 8 * half);
+              f32x16 far;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) far[i] = vq2;
+              far = __builtin_amdgcn_mfma_f32_32x32x2f32(k[0], vq0, far, 0, 0, 0);
+              far = __builtin_amdgcn_mfma_f32_32x32x2f32(k[1], vq1, far, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) s[16 * h + i] = fmaf(-q.slope, __builtin_amdgcn_sqrtf(far[i]), s[16 * h + i]);
+            }
+          } else {
+            add_voxel_bias<KT / 2>(q, s, [&](int i) {
+              const f32x4 p = spos[b][at(i)];
+              return Voxel{p[0], p[2], p[1]};
+            });
+          }
+        } else if (MODE == kAny && a.slopes) {
+          add_place_bias<KT / 2>(q, s, key);
         }
+        if (masked) hide<KT / 2>(q, s, key);
         float top = m;
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) top = fmaxf(top, s[i]);
@@ -299,7 +372,7 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T))) void k_attn_tile(
           }
       }
     }
-    if (MODE == kAny && a.k_pos && threadIdx.x < KT && k0 + KT < k_end) spos[b ^ 1][threadIdx.x] = next_voxel;
+    if (k0 + KT < k_end) keep_voxel(b ^ 1);
   }
 
   const float sum = l + __shfl_xor(l, 32);
@@ -347,6 +420,7 @@ void tile_mode(const AttnArgs& a, hipStream_t s) {
 template <typename T>
 void tile_t(const AttnArgs& a, hipStream_t s) {
   if (a.cap == 0.0f && !a.slopes) return tile_mode<T, kBare>(a, s);
+  if (a.k_pos) return tile_mode<T, kVoxel>(a, s);
   if constexpr (!std::is_same_v<T, _Float16>) {
     if (!a.slopes && a.cap <= kCapWithoutMaximum) return tile_mode<T, kCapped>(a, s);
   }

@@ -278,3 +278,23 @@ def test_operators_in_a_graph():
         got = [t.clone() for t in out]
         want = step()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {turn}"
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("where,spread,step", [(0, 100, 1), (1_000_000, 500, 1), (0, 1000, 8), (-70_000, 30_000, 1),
+                                               (0, 4000, 16), (5, 1182, 3), (0, 1 << 30, 1), (40, 1, 1)])
+def test_distances_of_voxels(where, spread, step, dtype):
+    """Scenes far from the origin, of all sizes and spacings: near voxels' distances stay exact."""
+    say(f"attention with voxels within {spread} of {where}, multiples of {step}, {dtype}")
+    g = torch.Generator(DEV).manual_seed(6)
+    for lens in ([300, 70], [1, 200], [3, 2]):
+        b = Batch(lens, lens, 4, 2, 32, dtype)
+        n = sum(lens)
+        pos = step * torch.randint(where // step - spread // step, where // step + spread // step + 1, (n, 4), device=DEV,
+                                   generator=g, dtype=torch.int32)
+        # half of the voxels are neighbours of others, so that small distances count
+        pos[n // 2:] = pos[:n - n // 2] + step * torch.randint(-1, 2, (n - n // 2, 4), device=DEV, generator=g, dtype=torch.int32)
+        b.q_pos = b.k_pos = pos
+        b.slopes = b.slopes * 200 / max(spread, 8)
+        b.check("voxels", bias="voxel")
+        b.check("voxels, causal and capped", bias="voxel", causal=True, cap=5.0)

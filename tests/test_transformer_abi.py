@@ -44,7 +44,8 @@ def linear(**kw):
     (dict(m=1 << 31), B.SPCONV_EUNSUPPORTED), (dict(x=None), B.SPCONV_EINVAL), (dict(xs=None), B.SPCONV_EINVAL),
     (dict(w=None), B.SPCONV_EINVAL), (dict(ws=None), B.SPCONV_EINVAL), (dict(y=None), B.SPCONV_EINVAL),
     (dict(x=P + 8), B.SPCONV_EINVAL), (dict(w=P + 8), B.SPCONV_EINVAL), (dict(y=P + 1), B.SPCONV_EINVAL),
-    (dict(xs=P + 1), B.SPCONV_EINVAL), (dict(m=0, x=None), B.SPCONV_OK), (dict(n=0, w=None, ld_y=0), B.SPCONV_OK),
+    (dict(xs=P + 1), B.SPCONV_EINVAL), (dict(ld_x=(1 << 23) + 16), B.SPCONV_EUNSUPPORTED),
+    (dict(ld_w=(1 << 23) + 16), B.SPCONV_EUNSUPPORTED), (dict(ld_xs=(1 << 21) + 1), B.SPCONV_EUNSUPPORTED), (dict(m=0, x=None), B.SPCONV_OK), (dict(n=0, w=None, ld_y=0), B.SPCONV_OK),
 ])
 def test_linear_refusals(kw, status):
     assert linear(**kw) == status
@@ -68,7 +69,7 @@ BAD = [
     (dict(scale=float("inf")), B.SPCONV_EINVAL), (dict(scale=float("nan")), B.SPCONV_EINVAL), (dict(cap=-1.0), B.SPCONV_EINVAL),
     (dict(cap=float("nan")), B.SPCONV_EINVAL), (dict(d_q_pos=P), B.SPCONV_EINVAL), (dict(d_q_pos=P, d_k_pos=P), B.SPCONV_EINVAL),
     (dict(n_q=1 << 31), B.SPCONV_EUNSUPPORTED), (dict(n_k=1 << 31), B.SPCONV_EUNSUPPORTED),
-    (dict(heads=65536, kv_heads=65536), B.SPCONV_EUNSUPPORTED),
+    (dict(heads=65536, kv_heads=65536), B.SPCONV_EUNSUPPORTED), (dict(max_k=(1 << 30) + 1), B.SPCONV_EUNSUPPORTED),
 ]
 
 
@@ -77,6 +78,7 @@ BAD = [
     (dict(d_out=None), B.SPCONV_EINVAL), (dict(d_q_start=None), B.SPCONV_EINVAL), (dict(d_k_start=None), B.SPCONV_EINVAL),
     (dict(d_q=P + 8), B.SPCONV_EINVAL), (dict(d_out=P + 8), B.SPCONV_EINVAL), (dict(q_row=252), B.SPCONV_EUNSUPPORTED),
     (dict(k_row=-128), B.SPCONV_EUNSUPPORTED), (dict(out_head=56), B.SPCONV_EINVAL), (dict(out_row=32), B.SPCONV_EINVAL),
+    (dict(k_row=(1 << 24) + 8), B.SPCONV_EUNSUPPORTED), (dict(v_row=(1 << 24) + 8), B.SPCONV_EUNSUPPORTED),
     (dict(max_q=0), B.SPCONV_EINVAL), (dict(n_q=0, d_q=None), B.SPCONV_OK), (dict(n_docs=0), B.SPCONV_OK),
 ])
 def test_attention_refusals(kw, status):
