@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       for (int i = 0; i < 8; ++i) sc[i] = s[n][i / 4][i % 4];
       const auto at = [&](int i) { return 16 * (i / 4) + 4 * g + i % 4; };
       const auto key = [&](int i) { return k0 + at(i); };
-      if (a.cap > 0.0f) cap_scores<8>(a, sc);
+      if (a.cap > 0.0f) cap_scores<8, E == 4>(a, sc);
       if (a.k_pos) {
         add_voxel_bias<8>(q[n], sc, [&](int i) {
           const f32x4 p = spos[wave][at(i)];

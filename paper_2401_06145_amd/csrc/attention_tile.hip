@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T), MODE)) void k_attn
       const bool masked = k0 + KT > lim_lo;
       const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
       if constexpr (MODE == kCapped) {
-        cap_scores<KT / 2>(a, s);
+        cap_scores<KT / 2, E == 4>(a, s);
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
         if (masked) {
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T), MODE)) void k_attn
         }
       } else {
         const auto key = [&](int i) { return k0 + at(i); };
-        if (MODE != kBare && a.cap > 0.0f) cap_scores<KT / 2>(a, s);
+        if (MODE != kBare && a.cap > 0.0f) cap_scores<KT / 2, E == 4>(a, s);
         if constexpr (MODE == kVoxel) {
           if (near_q && snear[b]) {
 #pragma unroll
