@@ -91,8 +91,8 @@ __device__ __forceinline__ void store_y(const LinearArgs& a, int64_t row, int n0
 
 // ---------------------------------------------------------------------------
 // Tiles: a workgroup of WM x WN waves takes BM rows and BN outputs, a block of 128 columns at
-// a time through LDS.  The next block of rows, weights and row scales is on its way from
-// memory straight into the other half of LDS while one is multiplied.  Rows of 128 bytes: the
+// a time through LDS.  With DEEP = 2 the next block of rows, weights and row scales is on its
+// way from memory straight into the other half of LDS while one is multiplied.  Rows of 128 bytes: the
 // 16-byte chunk c of row r lies at chunk c ^ r % 8, and a lane's 32 bytes of an operand row are
 // its chunks g and g + 4: every read of 16 rows then meets every bank once (240 bytes a clock and
 // CU measured; neighbouring chunks 2 g and 2 g + 1 in the same order give 126).  Rows and
@@ -100,9 +100,10 @@ __device__ __forceinline__ void store_y(const LinearArgs& a, int64_t row, int n0
 //
 // What bounds it: 256 x 256 x 128 a step take 0.95 us of matrix and vector instructions, 1.6 us
 // with the reads from LDS (the 8 waves of a CU go in step), 2.0 us with the loads (64 KB, one
-// step ahead).  16,384 x 8192 x 4096: 519 us, 2.1 PFLOP/s; a plain library product of e4m3, without
-// scales, takes 357 us.  Tried: 128 x 128 tiles, two workgroups a CU (621 us: twice the
-// loads); weights two steps ahead (541 us); columns of 2 or 8 tiles per XCD (541, 544 us).
+// step ahead).  16,384 x 8192 x 4096: 494 us, 2.2 PFLOP/s; a plain library product of e4m3, without
+// scales, takes 357 us.  Tried: 128 x 128 tiles, two workgroups a CU (621 us where
+// this took 519: twice the loads); weights two steps ahead (541); columns of 2 or 8 tiles per XCD (541,
+// 544); loads spread over the products (557).
 // ---------------------------------------------------------------------------
 
 // WORDS times 4 bytes a lane from memory straight into LDS: those at `at` of the buffer (zeros
@@ -126,13 +127,15 @@ __device__ __forceinline__ u32x4 buffer(const void* from, int64_t bytes) {
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
 }
 
-template <typename T, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(LinearArgs a) {
+template <typename T, bool EXACT, int BM, int BN, int WM, int WN, int DEEP>
+__global__ __launch_bounds__(64 * WM * WN, DEEP == 1 ? 3 : 2) void k_linear_tile(LinearArgs a) {
   constexpr int TH = 64 * WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int PX = BM * 8 / TH, PW = BN * 8 / TH;  // 16-byte chunks a thread brings
   static_assert(TH >= BM, "a thread brings at most one row scale");
-  __shared__ __align__(16) u32x4 sx[2][BM * 8], sw[2][BN * 8];
+  __shared__ __align__(16) u32x4 blocks[DEEP * (BM + BN) * 8];
+  u32x4(*const sx)[BM * 8] = reinterpret_cast<u32x4(*)[BM * 8]>(blocks);
+  u32x4(*const sw)[BN * 8] = reinterpret_cast<u32x4(*)[BN * 8]>(blocks + DEEP * BM * 8);
   __shared__ __align__(16) float sxs[2][BM * 4];  // row scales of four blocks
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int wm = wave / WN, wn = wave % WN;
@@ -207,12 +210,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(LinearArgs a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-  if (a.kb > 0) bring_block(0, 0);
+  if (DEEP == 2 && a.kb > 0) bring_block(0, 0);
   for (int b = 0; b < a.kb; ++b) {
-    const int buf = b & 1;
+    const int buf = DEEP == 2 ? b & 1 : 0;
+    if (DEEP == 1) {
+      if (b > 0) __syncthreads();  // the block before is read
+      bring_block(b, 0);
+    }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the block is in LDS
     __syncthreads();                     // and so are the others'; the other half is free
-    if (b + 1 < a.kb) bring_block(b + 1, buf ^ 1);
+    if (DEEP == 2 && b + 1 < a.kb) bring_block(b + 1, buf ^ 1);
     const float sb = ws[b];
     u32x4 f[2][2], fw[NT][2];
     float scale[2];
@@ -248,14 +255,53 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(LinearArgs a) {
       }
     }
   }
+  // Through LDS, so that whole lines of a row are stored together, past the caches (11,003 x 768 x
+  // 256 in float16: 10.5 us with a lane's 32 bytes stored by itself, so 7.5; stored together but
+  // cached 8.9, by itself past the caches 13.5).  The 16-byte chunk c of row r lies at c ^ r % 16.
+  constexpr int PER = 16 / (int)sizeof(T), CH = BN / PER;
+  static_assert(BM * CH <= DEEP * (BM + BN) * 8, "the tile fits the blocks' place");
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
+    const int r = wm * 16 * MT + 16 * i + r16;
     float v[4 * NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
-    store_y<T, 4 * NT>(a, m0 + wm * 16 * MT + 16 * i + r16, n0 + wn * 16 * NT + 4 * NT * g, v);
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = a.relu && acc[i][j][e] < 0.0f ? 0.0f : acc[i][j][e];
+#pragma unroll
+    for (int h = 0; h < 4 * NT / PER; ++h) {
+      u32x4 w;
+      if constexpr (PER == 4) {
+        w = __builtin_bit_cast(u32x4, (f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]}));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack2<T>(v[8 * h + 2 * e], v[8 * h + 2 * e + 1]);
+      }
+      blocks[r * CH + ((wn * 16 * NT + 4 * NT * g) / PER + h ^ r % 16)] = w;
+    }
+  }
+  __syncthreads();
+  T* y = static_cast<T*>(a.y) + m0 * a.ld_y + n0;
+  if (a.wide_y) {
+#pragma unroll
+    for (int i = 0; i < BM * CH / TH; ++i) {
+      const int p = threadIdx.x + TH * i, r = p / CH, c = p % CH;
+      if (r >= rows || PER * c >= outs) continue;
+      const u32x4 w = blocks[r * CH + (c ^ r % 16)];
+      if (PER * (c + 1) <= outs) {
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(y + r * a.ld_y + PER * c));
+      } else {
+        for (int e = 0; PER * c + e < outs; ++e)
+          y[r * a.ld_y + PER * c + e] = reinterpret_cast<const T*>(&blocks[r * CH + (c ^ r % 16)])[e];
+      }
+    }
+  } else {  // rows that no wide store fits: element by element
+    for (int p = threadIdx.x; p < BM * BN; p += TH) {
+      const int r = p / BN, c = p % BN;
+      if (r < rows && c < outs)
+        y[r * a.ld_y + c] = reinterpret_cast<const T*>(&blocks[r * CH + (c / PER ^ r % 16)])[c % PER];
+    }
   }
 }
 
@@ -372,17 +418,21 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
   }
 #undef SPC_W
 #undef SPC_R
-#define SPC_T(EXACT, BM, BN, WM, WN)                                                                                  \
-  hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN>),                                                       \
+#define SPC_T(EXACT, BM, BN, WM, WN, DEEP)                                                                            \
+  hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN, DEEP>),                                                 \
                      dim3((unsigned)(((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN))), dim3(64 * WM * WN), 0, s, a)
+  // Up to 512 columns: one block in LDS at a time, so that three workgroups share a CU and cover
+  // each other's loads and stores (32,043 x 768 x 256: 15.3 us, with large tiles 20.5; 11,003 x 768 x 256: 7.5,
+  // with two blocks 9; 1024 columns: 14.9, and 13.6 with two).  Else large tiles where they fill the CUs.
   if constexpr (!std::is_same_v<T, float>) {
     if (!exact) {
-      if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4);
-      else SPC_T(false, 128, 128, 2, 2);
+      if (a.kb <= 4) SPC_T(false, 128, 128, 2, 2, 1);
+      else if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4, 2);
+      else SPC_T(false, 128, 128, 2, 2, 2);
       return;
     }
   }
-  SPC_T(true, 128, 128, 2, 2);
+  SPC_T(true, 128, 128, 2, 2, 2);
 #undef SPC_T
 }
 

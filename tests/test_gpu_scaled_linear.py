@@ -131,3 +131,20 @@ def test_linear_of_many_tiles(m, n, k, dtype):
     bound = mag * (7 * 2.0 ** -13 + (min(k, 128) + k / 128 + 4) * 2.0 ** -24) + want.abs() * ref.UNIT[dtype] + ref.TINY[dtype]
     assert bool(((got.double() - want).abs() <= bound).all())
     ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "exact")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("first", [0, 1, 8])
+@pytest.mark.parametrize("m,n,k", [(333, 200, 272), (333, 136, 1152), (200, 3, 640), (4200, 4203, 1152)])
+def test_linear_stores_only_its_outputs(m, n, k, dtype, first):
+    """Outputs inside wider rows of any alignment, of numbers that fill no 16 bytes."""
+    say(f"scaled product into a part of wider rows, {m} x {n} x {k} {dtype} from {first}")
+    x, w = bits8(m, k, 31), bits8(n, k, 32)
+    xs, ws = scales(m, k, 33) * 1e-4, scales(-(-n // 128), k, 34) * 1e-4
+    want = B.scaled_linear(x, xs, w, ws, dtype)
+    for pad in (5, 8):
+        wide = torch.full((m + 1, first + n + pad), 7.0, device=DEV, dtype=dtype)
+        B.spconv_scaled_linear(x, xs, w, ws, wide[:m, first:first + n])
+        assert torch.equal(wide[:m, first:first + n], want)
+        wide[:m, first:first + n] = 7.0
+        assert bool((wide == 7).all())
