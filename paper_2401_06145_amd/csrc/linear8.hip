@@ -409,11 +409,22 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
     else SPC_R(MT, NT, WAVES);            \
   } while (0)
   if (few_rows(a)) {
-    if (a.m <= 16) SPC_W(1, 1, 16);
-    else if (a.m <= 32) SPC_W(2, 1, 16);
-    else if (a.m <= 48) SPC_W(3, 1, 16);
-    else if (a.m <= 64) SPC_W(4, 1, 16);
-    else SPC_R(4, 2, 8);
+    // As few rows a workgroup as one workgroup a CU allows: reading 16 (MT + NT) rows is what takes
+    // its time (64 x 1024 x 4096: 14.9 us with 64 rows a workgroup, 6.8 with 16).  Where the outputs alone
+    // fill the CUs twice, 32 of them a workgroup, as rows are then read half as often (64 x
+    // 8192 x 4096: 29.6 -> 18.1 us), but for one strip of rows 16 and shorter workgroups (1 x 8192 x 8192:
+    // 14.8 -> 13.6 us, with 32 outputs 19.7).
+    const auto fits = [&](int mt) { return (a.m + 16 * mt - 1) / (16 * mt) * ((a.n + 15) / 16) <= 256; };
+    const bool many = a.n > 4096;
+    if (many && a.m <= 16) SPC_W(1, 1, 8);
+    else if (many && a.m <= 32) SPC_W(2, 2, 8);
+    else if (many && a.m <= 48) SPC_W(3, 2, 8);
+    else if (many) SPC_W(4, 2, 8);
+    else if (a.m <= 16 || fits(1)) SPC_W(1, 1, 16);
+    else if (a.m <= 32 || fits(2)) SPC_W(2, 1, 16);
+    else if (a.m <= 48 || fits(3)) SPC_W(3, 1, 16);
+    else if (a.m <= 64 || fits(4)) SPC_W(4, 1, 16);
+    else SPC_W(4, 2, 8);
     return;
   }
 #undef SPC_W
