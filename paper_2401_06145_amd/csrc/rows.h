@@ -53,14 +53,15 @@ __device__ __forceinline__ void load8(const T* p, float* v) {
     for (int i = 0; i < 4; ++i) unpack2<T>(a[i], &v[2 * i], &v[2 * i + 1]);
   }
 }
+// Stored past the caches: rows that no other workgroup reads.
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const float* v) {
+__device__ __forceinline__ void store8_past(T* p, const float* v) {
   if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p) + 1);
   } else {
-    *reinterpret_cast<u32x4*>(p) =
-        u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+    const u32x4 w = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
   }
 }
 

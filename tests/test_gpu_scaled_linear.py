@@ -148,3 +148,14 @@ def test_linear_stores_only_its_outputs(m, n, k, dtype, first):
         assert torch.equal(wide[:m, first:first + n], want)
         wide[:m, first:first + n] = 7.0
         assert bool((wide == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(1, 4112, 2064), (20, 4200, 272), (40, 4111, 640), (64, 5000, 144), (33, 4097, 1536),
+                                   (64, 1024, 4096), (128, 1000, 3200), (250, 1024, 4096)])
+def test_linear_of_few_rows_and_many_outputs(m, n, k, dtype):
+    say(f"scaled product {m} x {n} x {k} {dtype}")
+    x, w = bits8(m, k, 41), bits8(n, k, 42)
+    xs, ws = scales(m, k, 43) * 1e-4, scales(-(-n // 128), k, 44) * 1e-4
+    want, mag = ref.scaled_linear(x, xs, w, ws)
+    ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "product")
