@@ -257,8 +257,9 @@ __global__ __launch_bounds__(64 * WM * WN, DEEP == 1 ? 3 : 2) void k_linear_tile
   }
   // Through LDS, so that whole lines of a row are stored together, past the caches (11,003 x 768 x
   // 256 in float16: 10.5 us with a lane's 32 bytes stored by itself, so 7.5; stored together but
-  // cached 8.9, by itself past the caches 13.5).  The 16-byte chunk c of row r lies at c ^ r % 16.
-  constexpr int PER = 16 / (int)sizeof(T), CH = BN / PER;
+  // cached 8.9, by itself past the caches 13.5).  The 16-byte chunk c of row r lies at c ^ r % 16
+  // (8, where a row has 8).
+  constexpr int PER = 16 / (int)sizeof(T), CH = BN / PER, SW = CH < 16 ? CH : 16;
   static_assert(BM * CH <= DEEP * (BM + BN) * 8, "the tile fits the blocks' place");
   __syncthreads();
 #pragma unroll
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(64 * WM * WN, DEEP == 1 ? 3 : 2) void k_linear_tile
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = pack2<T>(v[8 * h + 2 * e], v[8 * h + 2 * e + 1]);
       }
-      blocks[r * CH + ((wn * 16 * NT + 4 * NT * g) / PER + h ^ r % 16)] = w;
+      blocks[r * CH + ((wn * 16 * NT + 4 * NT * g) / PER + h ^ r % SW)] = w;
     }
   }
   __syncthreads();
@@ -288,19 +289,19 @@ __global__ __launch_bounds__(64 * WM * WN, DEEP == 1 ? 3 : 2) void k_linear_tile
     for (int i = 0; i < BM * CH / TH; ++i) {
       const int p = threadIdx.x + TH * i, r = p / CH, c = p % CH;
       if (r >= rows || PER * c >= outs) continue;
-      const u32x4 w = blocks[r * CH + (c ^ r % 16)];
+      const u32x4 w = blocks[r * CH + (c ^ r % SW)];
       if (PER * (c + 1) <= outs) {
         __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(y + r * a.ld_y + PER * c));
       } else {
         for (int e = 0; PER * c + e < outs; ++e)
-          y[r * a.ld_y + PER * c + e] = reinterpret_cast<const T*>(&blocks[r * CH + (c ^ r % 16)])[e];
+          y[r * a.ld_y + PER * c + e] = reinterpret_cast<const T*>(&blocks[r * CH + (c ^ r % SW)])[e];
       }
     }
   } else {  // rows that no wide store fits: element by element
     for (int p = threadIdx.x; p < BM * BN; p += TH) {
       const int r = p / BN, c = p % BN;
       if (r < rows && c < outs)
-        y[r * a.ld_y + c] = reinterpret_cast<const T*>(&blocks[r * CH + (c / PER ^ r % 16)])[c % PER];
+        y[r * a.ld_y + c] = reinterpret_cast<const T*>(&blocks[r * CH + (c / PER ^ r % SW)])[c % PER];
     }
   }
 }
@@ -388,12 +389,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_rows(LinearArgs a) {
 }
 
 // The few-row form reads every row for each 16 or 32 outputs, but shares out the columns: it
-// takes up to 64 rows, and more of them where the columns are many and one workgroup of
-// 64 rows x 32 outputs a CU does the whole (128 x 4096 x 4096 18.5 us against 26 of the tiles, 300 x
-// 1024 x 4096 18.0 against 26; two rounds take 33, and 8 blocks of columns are even).
-bool few_rows(const LinearArgs& a) {
-  return a.m <= 64 || (a.kb >= 24 && (a.m + 63) / 64 * ((a.n + 31) / 32) <= 256);
-}
+// takes up to 64 rows, and more of them where one workgroup of 64 rows x 32 outputs a CU does
+// the whole (float32; the best tiles in brackets: 281 x 143 x 672 5.1 us [7.4], 1000 x 256 x 2048 9.0
+// [11.8], 70 x 4096 x 2048 9.9 [11.7], 281 x 1024 x 672 5.1 [6.5]; beyond it 1000 x 1024 x 512 6.4 [5.6],
+// 2500 x 256 x 640 8.4 [5.9]).
+bool few_rows(const LinearArgs& a) { return a.m <= 64 || (a.m + 63) / 64 * ((a.n + 31) / 32) <= 256; }
 
 template <typename T>
 void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
@@ -432,18 +432,30 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
 #define SPC_T(EXACT, BM, BN, WM, WN, DEEP)                                                                            \
   hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN, DEEP>),                                                 \
                      dim3((unsigned)(((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN))), dim3(64 * WM * WN), 0, s, a)
+  // Tiles by how many of 128 x 128 there are.  Few leave CUs idle, for which smaller ones are
+  // worth their reads (bfloat16, tiles of 64 x 64, 64 x 128, 128 x 128: 1500 x 2048 x 1024, 192 of
+  // them: 8.3, 8.7, 9.9 us; 1000 x 1024 x 2048 9.1, 11.2, 14.9; 4000 x 1024 x 1024, 256 of them: 10.0, 8.8,
+  // 9.8; 3000 x 1500 x 4096, 288: 42.3, 34.7, 39.0; 4000 x 2048 x 1024, 512: 17.8, 16.8, 13.6).
+  //
   // Up to 512 columns: one block in LDS at a time, so that three workgroups share a CU and cover
   // each other's loads and stores (32,043 x 768 x 256: 15.3 us, with large tiles 20.5; 11,003 x 768 x 256: 7.5,
-  // with two blocks 9; 1024 columns: 14.9, and 13.6 with two).  Else large tiles where they fill the CUs.
+  // with two blocks 9; 1024 columns: 14.9, and 13.6 with two).  Float32 outputs of such a tile do
+  // not fit its one block; 64 x 128 does there (11,003 x 768 x 256: 11.6 against 15.6).  Else
+  // large tiles where they fill the CUs.
+  const int64_t tiles = ((a.m + 127) / 128) * ((a.n + 127) / 128);
   if constexpr (!std::is_same_v<T, float>) {
     if (!exact) {
-      if (a.kb <= 4) SPC_T(false, 128, 128, 2, 2, 1);
+      if (tiles <= 192) SPC_T(false, 64, 64, 2, 2, 2);
+      else if (tiles <= 384) SPC_T(false, 64, 128, 2, 2, 2);
+      else if (a.kb <= 4) SPC_T(false, 128, 128, 2, 2, 1);
       else if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4, 2);
       else SPC_T(false, 128, 128, 2, 2, 2);
       return;
     }
   }
-  SPC_T(true, 128, 128, 2, 2, 2);
+  if (tiles <= 192) SPC_T(true, 64, 64, 2, 2, 2);
+  else if (tiles <= 384 || a.kb <= 4) SPC_T(true, 64, 128, 2, 2, 2);
+  else SPC_T(true, 128, 128, 2, 2, 2);
 #undef SPC_T
 }
 
@@ -453,7 +465,7 @@ hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, in
                                 const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
                                 int relu, bool exact, hipStream_t s) {
   if (m <= 0 || n <= 0) return hipSuccess;
-  if (((m + 127) / 128) * ((n + 127) / 128) > 0x7fffffff) return hipErrorInvalidValue;
+  if (((m + 63) / 64) * ((n + 63) / 64) > 0x7fffffff) return hipErrorInvalidValue;
   ProfScope ps(KN_SCALED_LINEAR, s);
   const int64_t e = dtype == 0 ? 4 : 2;
   LinearArgs a = {static_cast<const uint8_t*>(x), xs, static_cast<const uint8_t*>(w), ws, y, ld_x, ld_xs, ld_w, ld_ws,

@@ -159,3 +159,24 @@ def test_linear_of_few_rows_and_many_outputs(m, n, k, dtype):
     xs, ws = scales(m, k, 43) * 1e-4, scales(-(-n // 128), k, 44) * 1e-4
     want, mag = ref.scaled_linear(x, xs, w, ws)
     ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "product")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(2100, 700, 272), (2100, 703, 1040), (3333, 1203, 144), (3333, 1200, 656), (2500, 3001, 272),
+                                   (2500, 3001, 784), (9000, 17, 528), (70, 4000, 256)])
+def test_linear_of_tiles_of_all_sizes(m, n, k, dtype):
+    """Against the product, and outputs inside wider rows that stay as they are."""
+    say(f"scaled product by tiles {m} x {n} x {k} {dtype}")
+    x, w = bits8(m, k, 51), bits8(n, k, 52)
+    xs, ws = scales(m, k, 53) * 1e-4, scales(-(-n // 128), k, 54) * 1e-4
+    want, mag = ref.scaled_linear(x, xs, w, ws)
+    ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "product")
+    got = B.scaled_linear(x, xs, w, ws, dtype, relu=True)
+    bound = mag * (7 * 2.0 ** -13 + (min(k, 128) + k / 128 + 4) * 2.0 ** -24) + want.abs() * ref.UNIT[dtype] + ref.TINY[dtype]
+    assert bool(((got.double() - want.relu()).abs() <= bound).all())
+    for first, pad in ((0, 5), (8, 8)):
+        wide = torch.full((m + 1, first + n + pad), 7.0, device=DEV, dtype=dtype)
+        B.spconv_scaled_linear(x, xs, w, ws, wide[:m, first:first + n], relu=True)
+        assert torch.equal(wide[:m, first:first + n], got)
+        wide[:m, first:first + n] = 7.0
+        assert bool((wide == 7).all())
