@@ -110,3 +110,19 @@ def test_norm_on_another_stream():
     y, _, _ = B.rms_norm(x, gamma, stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,c,pad,shift", [(37, 2, 0, 0), (35, 100, 0, 0), (18, 192, 1, 0), (19, 193, 0, 0), (7, 640, 0, 3),
+                                           (5, 641, 0, 0), (3, 4097, 0, 0), (7, 96, 0, 1), (9, 784, 0, 1)])
+def test_norm_of_any_width(n, c, pad, shift, dtype):
+    """Rows that no wide access fits, by as many lanes as their width asks for."""
+    say(f"norm of any width {n} x {c} {dtype}, pad {pad}, shift {shift}")
+    x, gamma = rows(n, c, dtype, 11, pad, shift), (1 + 0.2 * torch.randn(c, device=DEV)).to(dtype)
+    y, _, _ = B.rms_norm(x, gamma)
+    want, _ = ref.rms_norm(x, gamma)
+    ref.check_rows(y, want, c, "norm")
+    _, _, total = B.rms_norm(x, gamma, residual=x)
+    assert torch.equal(total, x + x)
+    if c % 16 == 0:
+        ref.check_bits8(*B.rms_norm(x, gamma, bits8=True)[:2], want, "8 bits")
