@@ -1121,6 +1121,11 @@ int check_attention(const spconv_attention_args* a) {
   return SPCONV_OK;
 }
 
+AttnPlan plan_of(const spconv_attention_args* a) {
+  return attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads, a->head_dim, a->dtype,
+                        a->causal != 0);
+}
+
 size_t attention_bytes(const spconv_attention_args* a, const AttnPlan& p, void* base, f32x2** ml, float** o) {
   if (p.splits <= 1) return 0;
   Bump b(base);
@@ -1187,8 +1192,7 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
 
 size_t spconv_attention_workspace_bytes(const spconv_attention_args* a) {
   if (check_attention(a) != SPCONV_OK) return 0;
-  return attention_bytes(a, attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads), nullptr,
-                         nullptr, nullptr);
+  return attention_bytes(a, plan_of(a), nullptr, nullptr, nullptr);
 }
 
 int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t ws_bytes, void* stream) {
@@ -1207,7 +1211,7 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
     return fail(SPCONV_EUNSUPPORTED, "rows of d_k and d_v at most 32 MiB apart");
   if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
     return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
-  const AttnPlan p = attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads);
+  const AttnPlan p = plan_of(a);
   AttnArgs k = {};
   const size_t need = attention_bytes(a, p, d_workspace, &k.part_ml, &k.part_o);
   if (need > 0 && (!d_workspace || ws_bytes < need)) return fail(SPCONV_ENOSPC, "attention workspace too small");

@@ -45,7 +45,8 @@ struct AttnPlan {
   int64_t slots;
   int splits, chunk;
 };
-AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads);
+AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads, int d, int dtype,
+                        bool causal);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 // attention_tile.hip, attention_rows.hip: the two forms.
 hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);

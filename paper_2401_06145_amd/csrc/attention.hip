@@ -17,7 +17,7 @@ namespace {
 using namespace attn;
 
 // Joins the results of up to FEW key ranges: a group of G lanes per row and head, four columns a
-// lane; all maxima and sums are read together, then all outputs (22,006 rows of 8 heads of 32, three
+// lane; all maxima and sums are read together, then all outputs (11,003 rows of 8 heads of 32, three
 // ranges: 34 us with a wave per row and head, 11 so).
 constexpr int kFewRanges = 8;
 template <typename T, int G>
@@ -129,22 +129,52 @@ void join_t(const AttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads) {
+// Key ranges of the many-query form: the number with the shortest estimated time.  A CU takes
+// `tile` us for 64 keys of 128 queries where it has one such workgroup, and `together` of that
+// for each where others cover its waits.  A launch lasts as long as its longest workgroup, or as all of
+// them on 256 CUs and a part of the longest behind them; joining costs a launch and the
+// partial outputs' way to memory and back, more than eight of them twice that.  (us, by 1, 2, 3, 4, 6, 8
+// ranges: 4096 queries of 8 heads of 128, causal, bfloat16 88, 77, 62, 73, 72, 78; 1024 of 32
+// heads of 64 20, 26, 26, 25, 28, 32; 1024 of 8 heads of 128 in float32 141, 80, 64, 49, 45, 55; voxels of two
+// frames, 11,003 of 8 heads of 32, 216, 191, 176, 185, 187, 194.)
+int tile_splits(int64_t groups, int64_t rows, int max_q, int max_k, int d, bool f32, bool causal) {
+  const float tile = f32 ? 0.066f * d : 0.5f + 0.006f * d, together = f32 ? 0.95f : 0.65f;
+  const float seen = causal ? std::max(0.5f, 1.0f - 0.5f * max_q / max_k) : 1.0f;
+  const int tiles = (max_k + 63) / 64;
+  const float all = groups * (tiles * seen) * tile * together / 256;
+  const float join = rows * d * 8.0f * seen / 4e6f;  // of one range
+  int best = 1;
+  float least = INFINITY;
+  for (int n = 1; n <= 32 && n <= tiles; ++n) {
+    const float longest = (tiles + n - 1) / n * tile;
+    const float us = std::max(longest, all + 0.7f * longest) + (n > 1 ? 5.0f + join * n * (n > kFewRanges ? 2 : 1) : 0.0f);
+    if (us < least) least = us, best = n;
+  }
+  return best;
+}
+
+AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads, int d, int dtype,
+                        bool causal) {
   AttnPlan p = {};
   const int group = heads / kv_heads;
   p.cols = (int64_t)max_q * group <= 64 ? max_q * group : 0;
   p.rows = p.cols > 0;
-  // the grid's third dimension holds the documents, or the key ranges
+  // the grid's third dimension holds the documents
   if (p.rows && n_docs > 65535) p.rows = false;
   p.slots = n_q / kQueryTile + n_docs;
-  const int64_t work = p.rows ? (int64_t)n_docs * kv_heads : (n_q / kQueryTile + std::min<int64_t>(n_docs, n_q)) * heads;
-  // Ranges of equal length: until a launch has about 3072 workgroups of the few-query form (48
-  // caches of up to 8192 keys, 8 key heads: 209 us with one range, 168 to 160 with 5 to 16, 178 with 22), or about
-  // 2048 of the other (voxels of two frames, 696 workgroups a range: 217 us with one or two,
-  // 199 with three, 209 with six), but of 256 keys at least (a document of 16,000 keys 24 us).
-  int64_t splits = ((p.rows ? 3072 : 2048) + work - 1) / std::max<int64_t>(work, 1);
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, max_k / 256));
-  p.chunk = (int)std::max<int64_t>(128, (((int64_t)max_k + splits - 1) / splits + 127) / 128 * 128);
+  int64_t splits, step;
+  if (p.rows) {
+    // Ranges of equal length until a launch has about 3072 workgroups (48 caches of up to 8192
+    // keys, 8 key heads: 209 us with one range, 168 to 160 with 5 to 16, 178 with 22), of 256 keys at least.
+    const int64_t work = std::max<int64_t>((int64_t)n_docs * kv_heads, 1);
+    splits = std::max<int64_t>(1, std::min<int64_t>((3072 + work - 1) / work, max_k / 256));
+    step = 128;
+  } else {
+    const int64_t tiles = n_q / kQueryTile + std::min<int64_t>(n_docs, n_q);
+    splits = tile_splits(tiles * heads, n_q * heads, max_q, max_k, d, dtype == 0, causal);
+    step = 64;
+  }
+  p.chunk = (int)std::max<int64_t>(step, (((int64_t)max_k + splits - 1) / splits + step - 1) / step * step);
   p.splits = std::max(1, (max_k + p.chunk - 1) / p.chunk);
   return p;
 }

@@ -15,10 +15,16 @@ using namespace attn;
 // What bounds it: memory.  48 caches of up to 8192 keys (8 key heads of 128, 16 bits, 801 MB) take
 // 156 to 160 us, 5.0 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
 // way (one: 183 us), except for rows of more than 256 bytes, whose registers would spill.
+// 32 and 64 columns a workgroup only where their sums fit its registers, else more workgroups
+// for a key head's columns (two documents of 49, 8 heads of 96, float32: 9.5 us, with 64 columns a
+// workgroup 42.8; a document of 11, two heads a key head of 256, bfloat16 9.2, with 32 22.7).
+constexpr int most_columns(int row) { return row <= 128 ? 64 : row <= 256 ? 32 : 16; }
+
 template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
-  constexpr int E = sizeof(T), ROW = D * E, KT = 32;
+  constexpr int E = sizeof(T), ROW = lds_columns(D) * E, KT = 32;
+  constexpr bool AHEAD = ROW < 1024;  // registers for the next tile while one is used
   typedef Lds<ROW> L;
   constexpr int P = KT * (int)L::CH / kWave;
   constexpr int STRIP = KT * ROW > D * 16 * 4 ? KT * ROW : D * 16 * 4;
@@ -28,11 +34,11 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 
   // Workgroups go around the 8 XCDs: each document and head begins with another range, or some
   // XCDs would get the ranges that only long documents fill (8 ranges of 48 caches: 219 us, so 160).
-  const int doc = blockIdx.z, kvh = blockIdx.y;
+  const int doc = blockIdx.z, kvh = blockIdx.y % a.kv_heads, col0 = blockIdx.y / a.kv_heads * 16 * NC;
   const int split = (blockIdx.x + doc + kvh) % a.splits;
   const Doc d = load_doc(a, doc);
   const int group = a.heads / a.kv_heads, cols = d.len_q * group;
-  if (cols <= 0) return;
+  if (cols <= col0) return;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, c16 = lane % 16, g = lane / 16;
   char* sv = strips[wave];
 
@@ -42,7 +48,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   int64_t row[NC];  // row of the packed queries times heads, plus the head
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
-    const int col = std::min(16 * n + c16, cols - 1), i = col / group, head = kvh * group + col % group;
+    const int col = std::min(col0 + 16 * n + c16, cols - 1), i = col / group, head = kvh * group + col % group;
     row[n] = (int64_t)(d.q0 + i) * a.heads + head;
     q[n] = make_query(a, d, i, head, origin);
     const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + i) * a.q_row + (int64_t)head * a.q_head;
@@ -99,12 +105,13 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
   };
   const int k_first = k_begin + wave * KT;
-  if (k_first < k_end) {
+  if (AHEAD && k_first < k_end) {
     fetch_v(k_first);
     fetch_k(k_first);
   }
   for (int k0 = k_first; k0 < k_end; k0 += 4 * KT) {
     const bool masked = k0 + KT > lim_lo;
+    if (!AHEAD) fetch_v(k0);
     bool bad = false;
     if (masked) {
 #pragma unroll
@@ -116,7 +123,8 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       const int p = lane + kWave * i, r = p / (int)L::CH, c = p % (int)L::CH;
       *reinterpret_cast<u32x4*>(sv + r * ROW + 16 * L::v_chunk16(r, c)) = rv[i];
     }
-    const bool more = k0 + 4 * KT < k_end;
+    const bool more = AHEAD && k0 + 4 * KT < k_end;
+    if (!AHEAD) fetch_k(k0);
     if (more) fetch_v(k0 + 4 * KT);
     const bool careful = masked && __any(bad);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       mine[t * kWave + lane] = v;
     }
     __syncthreads();
-    if (16 * n + c16 < cols) {
+    if (col0 + 16 * n + c16 < cols) {
       const int64_t part = (int64_t)split * a.n_q * a.heads + row[n];
       if (a.splits > 1 && wave == 0 && g == 0) a.part_ml[part] = f32x2{top, sum};
       const float inv = 1.0f / sum;
@@ -277,16 +285,20 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 
 template <typename T>
 hipError_t rows_t(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-  const dim3 grid((unsigned)a.splits, (unsigned)a.kv_heads, (unsigned)a.n_docs);
-#define SPC_D(D, NC) hipLaunchKernelGGL((k_attn_rows<T, D, NC>), grid, dim3(256), 0, s, a)
-#define SPC_C(D)                      \
-  do {                                \
-    if (p.cols <= 16) SPC_D(D, 1);      \
-    else if (p.cols <= 32) SPC_D(D, 2); \
-    else SPC_D(D, 4);                   \
+#define SPC_D(D, NC)                                                                                                \
+  hipLaunchKernelGGL((k_attn_rows<T, D, NC>),                                                                       \
+                     dim3((unsigned)a.splits, (unsigned)(a.kv_heads * ((p.cols + 16 * NC - 1) / (16 * NC))), \
+                        (unsigned)a.n_docs), dim3(256), 0, s, a)
+#define SPC_C(D)                                                                      \
+  do {                                                                                \
+    constexpr int most = most_columns(lds_columns(D) * (int)sizeof(T));               \
+    if (most == 16 || p.cols <= 16) SPC_D(D, 1);                                      \
+    else if (most == 32 || p.cols <= 32) SPC_D(D, (most < 32 ? 1 : 2));               \
+    else SPC_D(D, (most < 64 ? 1 : 4));                                               \
   } while (0)
   if (a.d <= 32) SPC_C(32);
   else if (a.d <= 64) SPC_C(64);
+  else if (a.d <= 96) SPC_C(96);
   else if (a.d <= 128) SPC_C(128);
   else SPC_C(256);
 #undef SPC_C

@@ -73,9 +73,9 @@ struct Near {
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
 // where the call is causal) start first.
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, waves_a_simd(D * sizeof(T), MODE)) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)) void k_attn_tile(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
-  constexpr int QT = kQueryTile, E = sizeof(T), ROW = D * E;
+  constexpr int QT = kQueryTile, E = sizeof(T), ROW = lds_columns(D) * E;
   constexpr int KT = ROW >= 1024 ? 32 : 64;
   // Rows of 256 bytes leave registers for operands ahead of their use: all of a tile of K before
   // the first product, a strip of V while the exponentials are computed (784 -> 770 us on whole
@@ -412,6 +412,7 @@ void tile_mode(const AttnArgs& a, hipStream_t s) {
 #define SPC_D(D) hipLaunchKernelGGL((k_attn_tile<T, D, MODE>), grid, dim3(256), 0, s, a)
   if (a.d <= 32) SPC_D(32);
   else if (a.d <= 64) SPC_D(64);
+  else if (a.d <= 96) SPC_D(96);
   else if (a.d <= 128) SPC_D(128);
   else SPC_D(256);
 #undef SPC_D

@@ -298,3 +298,24 @@ def test_distances_of_voxels(where, spread, step, dtype):
         b.slopes = b.slopes * 200 / max(spread, 8)
         b.check("voxels", bias="voxel")
         b.check("voxels, causal and capped", bias="voxel", causal=True, cap=5.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("d", [64, 72, 96, 128, 256])
+def test_key_heads_with_many_queries(d, dtype):
+    """17 to 64 queries of one key head, whole documents and caches, over one range of keys and several."""
+    say(f"attention, many queries of a key head, {d} columns, {dtype}")
+    for ql, kl, heads, kv, room in [([5, 3], [40, 3], 8, 1, 0), ([1, 1, 1], [700, 0, 33], 24, 1, 800), ([49, 20], [49, 1100], 2, 2, 0),
+                                    ([3, 2], [1300, 600], 34, 2, 1300)]:
+        b = Batch(ql, kl, heads, kv, d, dtype, room=room, seed=d)
+        b.check(f"{ql} {kl}", causal=True)
+        b.check(f"{ql} {kl}, all of it", causal=True, prefix=[n // 3 for n in kl], cap=20.0, bias="position")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens,heads,d", [([700, 64], 2, 96), ([300, 300, 5], 4, 256), ([1500], 1, 32), ([90] * 40, 8, 64)])
+def test_whole_documents_over_ranges_of_keys(lens, heads, d, dtype):
+    say(f"attention of whole documents {lens[:3]}, {heads} heads of {d}, {dtype}")
+    b = Batch(lens, lens, heads, heads, d, dtype, seed=7)
+    b.check("causal", causal=True)
+    b.check("voxels", bias="voxel")
