@@ -43,7 +43,7 @@ def _torch_ops() -> str:
     cmd = [HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__",
            "-I", INCLUDE, "-isystem", os.path.join(torch, "include"), "-isystem", "/opt/rocm/include",
            "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "torch_ops.cpp"), "-o", tmp,
-           "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+           "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for torch_ops.cpp:\n{r.stderr}")

@@ -1,10 +1,11 @@
 // The transformer operators for torch tensors: checks of the arguments, the outputs' memory and
 // the current stream, then one call of the C-ABI.  A binding in C++ because a new token's
 // kernels take about 3 us each: argument checks, allocations and the call from Python
-// (ctypes) took 9 to 13 us, and take 4 to 7 here.
+// (ctypes) took 9 to 13 us, and take 4 to 8 here.
 #include <Python.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/core/Tensor.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -104,7 +105,7 @@ void same_device(const at::Tensor& first, std::initializer_list<const at::Tensor
 }
 void* stream_of(const at::Tensor& t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 at::Tensor empty(at::IntArrayRef size, at::ScalarType dtype, const at::Tensor& like) {
-  return at::empty(size, like.options().dtype(dtype).requires_grad(false));
+  return at::Tensor(at::detail::empty_cuda(size, dtype, like.device(), std::nullopt));
 }
 
 // The library's status as a Python error; whether there is one.
