@@ -314,12 +314,12 @@ int spconv_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64
  *   d_x [m][k], d_w [n][k] e4m3 bytes (spconv_rms_norm writes such rows);
  *   d_x_scale [m][ceil(k / 128)], d_w_scale [ceil(n / 128)][ceil(k / 128)] float32;
  *   d_y [m][n] in `dtype`; relu != 0 applies max(0, .).
- * Scaled products and their sums are float32.  In 16-bit types, and more than 64 rows, a block's
- * 128 products are summed by the 8-bit matrix instruction, which drops a product 2^13 times
- * smaller than the largest of its group of eight, unless exact != 0: then, as for SPCONV_F32
- * and few rows always, they are summed in float32, at about half the speed.  k, ld_x and ld_w multiples of 16 (16-byte rows;
- * SPCONV_EUNSUPPORTED otherwise), rows of d_x, d_w and d_x_scale at most 8 MiB apart, d_x and d_w
- * 16-byte aligned; any m and n.  k = 0 gives zeros.
+ * Scaled products and their sums are float32.  In 16-bit types a block's 128 products are summed
+ * by the 8-bit matrix instruction, which drops a product 2^13 times smaller than the largest of
+ * its group of eight, unless exact != 0: then, as for SPCONV_F32 and for few rows or outputs
+ * always, they are summed in float32, at about half the speed.  k, ld_x and ld_w multiples of 16
+ * (16-byte rows; SPCONV_EUNSUPPORTED otherwise), rows of d_x, d_w and d_x_scale at most 8 MiB
+ * apart, d_x and d_w 16-byte aligned; any m and n.  k = 0 gives zeros.
  * d_y must not overlap the inputs. */
 int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, int64_t ld_x_scale,
                          const void* d_w, int64_t ld_w, const float* d_w_scale, int64_t ld_w_scale, void* d_y,
@@ -367,8 +367,8 @@ typedef struct {
   float scale, cap; /* cap 0: scores are not capped */
 } spconv_attention_args;
 
-/* Device workspace of spconv_attention: partial results where a launch with few queries splits
- * its keys; 0 where none are needed (and for invalid arguments).  Goes by sizes only, not by
+/* Device workspace of spconv_attention: partial results where a launch splits its keys; 0 where
+ * none are needed (and for invalid arguments).  Goes by sizes, type and causal only, not by
  * pointers.  256-byte aligned; calls whose work may overlap need a workspace each. */
 size_t spconv_attention_workspace_bytes(const spconv_attention_args* args);
 int spconv_attention(const spconv_attention_args* args, void* d_workspace, size_t ws_bytes, void* stream);
