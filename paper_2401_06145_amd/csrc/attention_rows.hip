@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   // loads are under way for the rest of the work on this one.
   Frag fk[2][D / 32];
   u32x4 rv[P];
-  Voxel pos = {0, 0, 0};
+  int32_t pos[4] = {0, 0, 0, 0};
   const auto fetch_k = [&](int k0) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -99,9 +99,9 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       if (k0 + r < d.len_k && c * (16 / E) < a.d)
         rv[i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
     }
-    if (a.k_pos && lane < KT) {
-      pos = Voxel{0, 0, 0};
-      if (k0 + lane < d.len_k) pos = voxel_from(a.k_pos + 4 * (d.k0 + k0 + lane), origin);
+    if (a.k_pos && lane < KT && k0 + lane < d.len_k) {
+#pragma unroll
+      for (int i = 1; i < 4; ++i) pos[i] = a.k_pos[4 * (d.k0 + k0 + lane) + i];
     }
   };
   const int k_first = k_begin + wave * KT;
@@ -117,7 +117,10 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
       for (int i = 0; i < P; ++i) bad |= odd_values<T>(rv[i]);
     }
-    if (a.k_pos && lane < KT) spos[wave][lane] = f32x4{pos.x, pos.y, pos.z, 0};
+    if (a.k_pos && lane < KT) {  // keys that do not exist are hidden, wherever they are
+      const Voxel v = voxel_from(pos, origin);
+      spos[wave][lane] = f32x4{v.x, v.y, v.z, 0};
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int p = lane + kWave * i, r = p / (int)L::CH, c = p % (int)L::CH;

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   constexpr int P = KT * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
   __shared__ __align__(16) char sk[2][KT * ROW], sv[2][KT * ROW];
   __shared__ f32x4 spos[2][KT];       // voxels of the keys: x, z, y, x^2 + y^2 + z^2
-  __shared__ uint32_t snear[2], sbits;  // whether they all are near; bits of the queries' voxels
+  __shared__ uint32_t snear[2], sbits[4];  // whether they all are near; bits of the waves' queries' voxels
   __shared__ uint32_t odd_at[3 * KT * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
 
   // which slot, head and range of keys
@@ -152,31 +152,41 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   bool near_q = false;
   if constexpr (MODE == kVoxel) {
     const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + std::min(row, d.len_q - 1));
-    if (threadIdx.x == 0) sbits = 0;
+    const uint32_t bits = ((uint32_t)p[1] - (uint32_t)origin[1]) | ((uint32_t)p[2] - (uint32_t)origin[2]) |
+                          ((uint32_t)p[3] - (uint32_t)origin[3]);
+    uint32_t all = 1u << 4;  // 16 is the spacing of the coarsest level
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all |= __any(bits >> i & 1) ? 1u << i : 0;
+    if (lane == 0) sbits[wave] = all;
     __syncthreads();
-    atomicOr(&sbits, ((uint32_t)p[1] - (uint32_t)origin[1]) | ((uint32_t)p[2] - (uint32_t)origin[2]) |
-                         ((uint32_t)p[3] - (uint32_t)origin[3]));
-    __syncthreads();
-    near.shift = __builtin_ctz(sbits | 1u << 4);  // 16 is the spacing of the coarsest level
+    near.shift = __builtin_ctz(sbits[0] | sbits[1] | sbits[2] | sbits[3]);
     near_q = __all(near(p, origin));
   }
-  f32x4 voxel;
-  bool voxel_near;
+  // Loaded beside a tile, looked at when the tile before is done: looked at at once, all of the
+  // tile's loads were awaited (voxels of two frames 177 us, so 170).
+  int32_t voxel[4] = {0, 0, 0, 0};
+  int voxels = 0;
   const auto fetch_voxel = [&](int k0) {
-    voxel = f32x4{0, 0, 0, 0};
-    voxel_near = true;
-    if (MODE == kVoxel && threadIdx.x < KT && k0 + (int)threadIdx.x < d.len_k) {
-      const int32_t* p = a.k_pos + 4 * (d.k0 + k0 + threadIdx.x);
-      const Voxel v = voxel_from(p, origin);
-      voxel = f32x4{v.x, v.z, v.y, fmaf(v.x, v.x, fmaf(v.y, v.y, v.z * v.z))};
-      voxel_near = near(p, origin);
+    voxels = MODE == kVoxel ? d.len_k - k0 : 0;
+    if ((int)threadIdx.x < std::min(KT, voxels)) {
+#pragma unroll
+      for (int i = 1; i < 4; ++i) voxel[i] = a.k_pos[4 * (d.k0 + k0 + threadIdx.x) + i];
     }
   };
   const auto keep_voxel = [&](int b) {
     if (MODE == kVoxel && wave == 0) {
-      if (lane < KT) spos[b][lane] = voxel;
-      const bool all = __all(voxel_near);
-      if (lane == 0) snear[b] = all;
+      bool ok = true;
+      if (lane < KT) {
+        f32x4 at = {0, 0, 0, 0};
+        if (lane < voxels) {
+          const Voxel v = voxel_from(voxel, origin);
+          at = f32x4{v.x, v.z, v.y, fmaf(v.x, v.x, fmaf(v.y, v.y, v.z * v.z))};
+          ok = near(voxel, origin);
+        }
+        spos[b][lane] = at;
+      }
+      ok = __all(ok);
+      if (lane == 0) snear[b] = ok;
     }
   };
   // this lane's part of the second operand of the distances, and |q|^2
