@@ -1233,6 +1233,10 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   k.poly_most = by >= 1e-4f && by <= 1e4f ? 0.5f / by : -1.0f;
   static const double kFit[2][5] = {{0.9999976762, -0.333206552, 0.131451455, -0.04337247954, 0.0},
                                     {0.9999999316, -0.3333277618, 0.1332057066, -0.05276212995, 0.01673756559}};
+  // and with two terms for |u| <= 0.11, within 1.3e-7 too
+  k.low_most = k.poly_most * 0.22f;
+  k.low[0] = (float)(0.99999394 * k.cap_log2 * by);
+  k.low[1] = (float)(-0.33132737 * k.cap_log2 * std::pow((double)by, 3));
   for (int i = 0; i < 5; ++i)
     k.poly[i] = (float)(kFit[a->dtype == SPCONV_F32][i] * k.cap_log2 * std::pow((double)by, 2 * i + 1));
   k.slope_by = a->cap > 0.0f ? kLog2e : 1.0f / a->scale;

@@ -27,6 +27,7 @@ struct AttnArgs {
   float cap;         // > 0: scores are capped
   float cap_log2;    // cap log2(e)
   float tanh_by;     // 2 log2(e) scale / cap
+  float low[2], low_most;    // capped scores of products up to low_most, the same with two terms (16-bit rows)
   float poly[5], poly_most;  // capped scores of products up to poly_most, as an odd polynomial of them
   float slope_by;    // from the slopes' units to the scores'
   float exp_by;      // from the scores' units to log2

@@ -185,11 +185,12 @@ struct Query {
 };
 
 // cap tanh(u), u = scale s / cap, in units of log2.  Where every product of the wave is small
-// (|u| <= 1/2: most scores, as caps are meant for the few large ones) by an odd polynomial of
-// degree 7 fitted to tanh there, within 1.3e-7 (FINE, for float32 rows: degree 9, 3e-9, as
-// the error counts times the cap); else as tanh(u) = 1 - 2 / (1 + e^{2u}), with its exact
-// limits, within 1.2e-7.  5 instructions instead of 3 and two transcendental ones, which take
-// twice as long (whole documents, cap 50: 855 -> 782 us).
+// (most are, as caps are meant for the few large ones) by an odd polynomial fitted to tanh
+// there: of degree 3 for |u| <= 0.11 and 7 for |u| <= 1/2, both within 1.3e-7 (FINE, for float32
+// rows: degree 9, 3e-9, as the error counts times the cap); else as tanh(u) =
+// 1 - 2 / (1 + e^{2u}), with its exact limits, within 1.2e-7.  3 or 5 instructions instead of 3
+// and two transcendental ones, which take twice as long (whole documents, cap 50: 855 us, 767 with
+// degree 7, 719 to 735 with 3; a cap of 20, whose scores are not that small, is even).
 template <bool FINE>
 __device__ __forceinline__ float small_cap(const AttnArgs& a, float s) {
   const float z = s * s;
@@ -201,7 +202,10 @@ __device__ __forceinline__ void cap_scores(const AttnArgs& a, float* s) {
   float most = 0.0f;
 #pragma unroll
   for (int i = 0; i < COUNT; ++i) most = fmaxf(most, fabsf(s[i]));
-  if (!__any(most > a.poly_most)) {
+  if (!FINE && !__any(most > a.low_most)) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i] *= fmaf(s[i] * s[i], a.low[1], a.low[0]);
+  } else if (!__any(most > a.poly_most)) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) s[i] = small_cap<FINE>(a, s[i]);
   } else {

@@ -319,3 +319,18 @@ def test_whole_documents_over_ranges_of_keys(lens, heads, d, dtype):
     b = Batch(lens, lens, heads, heads, d, dtype, seed=7)
     b.check("causal", causal=True)
     b.check("voxels", bias="voxel")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("spread", [0.02, 0.5, 1.0, 2.5, 12.0])
+def test_capped_scores_of_all_sizes(spread, dtype):
+    """Scores far below the cap, near it and above: each way to compute the hyperbolic tangent."""
+    say(f"attention with capped scores {spread} {dtype}")
+    for ql, kl in (([150, 40], [150, 333]), ([1, 3], [700, 90])):
+        b = Batch(ql, kl, 4, 2, 64, dtype, spread=spread, seed=11)
+        for cap in (2.0, 10.0, 50.0):
+            got = b.run(causal=True, cap=cap)
+            want, mag = ref.attention(b.q, b.k, b.v, b.q_lens, b.k_lens, causal=True, cap=cap)
+            u = ref.UNIT[dtype]  # float32 errors of the scores grow with them
+            bound = mag * (2 * u + 4e-5 * max(1.0, spread)) + want.abs() * u + ref.TINY[dtype]
+            assert bool(((got.double() - want).abs() <= bound).all()), f"cap {cap}"
