@@ -136,7 +136,7 @@ void join_t(const AttnArgs& a, hipStream_t s) {
 // partial outputs' way to memory and back, more than eight of them twice that.  (us, by 1, 2, 3, 4, 6, 8
 // ranges: 4096 queries of 8 heads of 128, causal, bfloat16 88, 77, 62, 73, 72, 78; 1024 of 32
 // heads of 64 20, 26, 26, 25, 28, 32; 1024 of 8 heads of 128 in float32 141, 80, 64, 49, 45, 55; voxels of two
-// frames, 11,003 of 8 heads of 32, 213, 185, 170, 176, 175, 177.)
+// frames, 11,003 of 8 heads of 32, 199, 170, 159, 164, 164, 165.)
 int tile_splits(int64_t groups, int64_t rows, int max_q, int max_k, int d, bool f32, bool causal) {
   const float tile = f32 ? 0.066f * d : 0.5f + 0.006f * d, together = f32 ? 0.95f : 0.65f;
   const float seen = causal ? std::max(0.5f, 1.0f - 0.5f * max_q / max_k) : 1.0f;

@@ -65,9 +65,13 @@ struct Near {
   }
 };
 
-// A workgroup of four waves takes 128 queries of one head and one range of keys, KT keys at a
-// time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
+// A workgroup of four waves takes 128 queries of one head and one range of keys, KT or 2 KT
+// keys at a time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
 // from memory straight into the other half of LDS while one is multiplied.
+//
+// What bounds it: the vector and the matrix unit, each busy for 45 % of the cycles (documents of
+// up to 8192, 16 heads of 128, capped: 708 to 740 us, 0.94 PFLOP/s); with voxels and short rows
+// the vector unit: a root, an exponential and eight more instructions a score (159 us).
 //
 // Workgroups with the same key head are neighbours in time on one XCD (workgroups go around
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
@@ -84,11 +88,15 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   constexpr bool AHEAD = ROW == 256 && MODE < kVoxel;
   constexpr int VA = AHEAD ? 1 : 0;
   typedef Lds<ROW> L;
-  constexpr int P = KT * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
-  __shared__ __align__(16) char sk[2][KT * ROW], sv[2][KT * ROW];
-  __shared__ f32x4 spos[2][KT];       // voxels of the keys: x, z, y, x^2 + y^2 + z^2
-  __shared__ uint32_t snear[2], sbits[4];  // whether they all are near; bits of the waves' queries' voxels
-  __shared__ uint32_t odd_at[3 * KT * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
+  // Keys between two barriers: two tiles for short rows with voxels, whose coordinates one or two
+  // waves prepare while the others wait (two frames, 8 heads of 32: 169 us, so 159; of 64
+  // 125, so 119; without voxels it is even, and longer rows would lose a workgroup a CU).
+  constexpr int KB = MODE == kVoxel && ROW <= 128 ? 2 * KT : KT;
+  constexpr int P = KB * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
+  __shared__ __align__(16) char sk[2][KB * ROW], sv[2][KB * ROW];
+  __shared__ f32x4 spos[2][KB];       // voxels of the keys: x, z, y, x^2 + y^2 + z^2
+  __shared__ uint32_t snear[2][KB / KT], sbits[4];  // whether they all are near; bits of the waves' queries' voxels
+  __shared__ uint32_t odd_at[3 * KB * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
 
   // which slot, head and range of keys
   const int per = a.heads * a.slots, split = blockIdx.x / per, in = blockIdx.x - split * per;
@@ -143,7 +151,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
     at_v[i] = cv * (16 / E) < a.d ? r * v_bytes + 16 * cv : INT32_MIN;
   }
   const auto bring = [&](int k0, int b) {
-    const int rows = std::min(d.len_k - k0, KT);
+    const int rows = std::min(d.len_k - k0, KB);
     bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
     bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
   };
@@ -168,25 +176,26 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   int voxels = 0;
   const auto fetch_voxel = [&](int k0) {
     voxels = MODE == kVoxel ? d.len_k - k0 : 0;
-    if ((int)threadIdx.x < std::min(KT, voxels)) {
+    if ((int)threadIdx.x < std::min(KB, voxels)) {
 #pragma unroll
       for (int i = 1; i < 4; ++i) voxel[i] = a.k_pos[4 * (d.k0 + k0 + threadIdx.x) + i];
     }
   };
   const auto keep_voxel = [&](int b) {
-    if (MODE == kVoxel && wave == 0) {
+    static_assert(KT == 64 || MODE != kVoxel || KB == KT, "a wave looks at one tile");
+    if (MODE == kVoxel && (int)threadIdx.x < (KB + 63) / 64 * 64) {
       bool ok = true;
-      if (lane < KT) {
+      if ((int)threadIdx.x < KB) {
         f32x4 at = {0, 0, 0, 0};
-        if (lane < voxels) {
+        if ((int)threadIdx.x < voxels) {
           const Voxel v = voxel_from(voxel, origin);
           at = f32x4{v.x, v.z, v.y, fmaf(v.x, v.x, fmaf(v.y, v.y, v.z * v.z))};
           ok = near(voxel, origin);
         }
-        spos[b][lane] = at;
+        spos[b][threadIdx.x] = at;
       }
       ok = __all(ok);
-      if (lane == 0) snear[b] = ok;
+      if (lane == 0) snear[b][wave] = ok;
     }
   };
   // this lane's part of the second operand of the distances, and |q|^2
@@ -199,39 +208,43 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
     keep_voxel(0);
   }
   int b = 0;
-  for (int k0 = k_begin; k0 < k_end; k0 += KT, b ^= 1) {
+  const int last = std::min(lim_hi, k_end);  // behind it there is nothing for this wave
+  for (int kb = k_begin; kb < k_end; kb += KB, b ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile is in LDS
     __syncthreads();                     // and so are the others'; the other half is free
     // A hidden key's value is multiplied by 0, which must not make an infinity or a NaN of it
     // part of the sum.  Where a tile with hidden keys has such values they leave the tile, and
     // go to the queries that see them after the product.
     bool odd = false;
-    if (k0 + KT > tile_lo) {
+    if (kb + KB > tile_lo) {
 #pragma unroll
       for (int i = 0; i < P; ++i)
         odd |= odd_values<T>(*reinterpret_cast<const u32x4*>(sv[b] + 16 * (threadIdx.x + 256 * i)));
       odd = __syncthreads_or(odd);
       if (odd) {
-        for (int i = threadIdx.x; i < 3 * KT * (D / 32); i += 256) odd_at[i] = 0;
+        for (int i = threadIdx.x; i < 3 * KB * (D / 32); i += 256) odd_at[i] = 0;
         __syncthreads();
-        for (uint32_t p = threadIdx.x; p < KT * L::CH; p += 256) {
+        for (uint32_t p = threadIdx.x; p < KB * L::CH; p += 256) {
           const int r = p / L::CH, x = L::v_chunk(r, p % L::CH) * (16 / E);
           for (int j = 0; j < 16 / E; ++j) {
             T* v = reinterpret_cast<T*>(sv[b] + 16 * p) + j;
             const int kind = odd_kind((float)*v);
             if (kind < 0) continue;
-            atomicOr(&odd_at[(kind * KT + r) * (D / 32) + (x + j) / 32], 1u << ((x + j) % 32));
+            atomicOr(&odd_at[(kind * KB + r) * (D / 32) + (x + j) / 32], 1u << ((x + j) % 32));
             *v = (T)0.0f;
           }
         }
         __syncthreads();
       }
     }
-    if (k0 + KT < k_end) {
-      bring(k0 + KT, b ^ 1);
-      fetch_voxel(k0 + KT);
+    if (kb + KB < k_end) {
+      bring(kb + KB, b ^ 1);
+      fetch_voxel(kb + KB);
     }
-    if (k0 < lim_hi) {  // else nothing for this wave
+#pragma unroll 1
+    for (int k0 = kb; k0 < std::min(kb + KB, last); k0 += KT) {
+      const int sub = (k0 - kb) / KT;
+      const char *const tk = sk[b] + sub * KT * ROW, *const tv = sv[b] + sub * KT * ROW;
       float s[KT / 2];
       {
         f32x16 acc[KT / 32];
@@ -243,11 +256,11 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
           const int r = 32 * h + c32;
           if constexpr (E == 4) {
             const int c = 4 * k + 2 * half;
-            const f32x4 x = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c));
-            const f32x4 y = *reinterpret_cast<const f32x4*>(sk[b] + r * ROW + 16 * L::k_chunk(r, c + 1));
+            const f32x4 x = *reinterpret_cast<const f32x4*>(tk + r * ROW + 16 * L::k_chunk(r, c));
+            const f32x4 y = *reinterpret_cast<const f32x4*>(tk + r * ROW + 16 * L::k_chunk(r, c + 1));
             return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
           } else {
-            return *reinterpret_cast<const Frag*>(sk[b] + r * ROW + 16 * L::k_chunk(r, 2 * k + half));
+            return *reinterpret_cast<const Frag*>(tk + r * ROW + 16 * L::k_chunk(r, 2 * k + half));
           }
         };
         if constexpr (AHEAD) {
@@ -277,7 +290,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int r = 16 * c + 8 * (j / 4) + 4 * half + j % 4, x = 32 * t + c32;
-            f[j] = *reinterpret_cast<const float*>(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 4) + 4 * (x % 4));
+            f[j] = *reinterpret_cast<const float*>(tv + r * ROW + 16 * L::v_chunk(r, x / 4) + 4 * (x % 4));
           }
         } else {
           const int i = lane % 16, x = 32 * t + 16 * (lane / 16 % 2) + 4 * (i % 4);
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int r = 16 * c + 8 * j + 4 * half + i / 4;
-            w[j] = read_columns(sv[b] + r * ROW + 16 * L::v_chunk(r, x / 8) + 2 * (x % 8));
+            w[j] = read_columns(tv + r * ROW + 16 * L::v_chunk(r, x / 8) + 2 * (x % 8));
           }
           f = __builtin_bit_cast(Frag, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
@@ -314,10 +327,10 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
         const auto key = [&](int i) { return k0 + at(i); };
         if (MODE != kBare && a.cap > 0.0f) cap_scores<KT / 2, E == 4>(a, s);
         if constexpr (MODE == kVoxel) {
-          if (near_q && snear[b]) {
+          if (near_q && snear[b][sub]) {
 #pragma unroll
             for (int h = 0; h < KT / 32; ++h) {
-              const f32x2 k = *reinterpret_cast<const f32x2*>(reinterpret_cast<const char*>(&spos[b][32 * h + c32]) + 8 * half);
+              const f32x2 k = *reinterpret_cast<const f32x2*>(reinterpret_cast<const char*>(&spos[b][sub * KT + 32 * h + c32]) + 8 * half);
               f32x16 far;
 #pragma unroll
               for (int i = 0; i < 16; ++i) far[i] = vq2;
@@ -328,7 +341,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
             }
           } else {
             add_voxel_bias<KT / 2>(q, s, [&](int i) {
-              const f32x4 p = spos[b][at(i)];
+              const f32x4 p = spos[b][sub * KT + at(i)];
               return Voxel{p[0], p[2], p[1]};
             });
           }
@@ -374,7 +387,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll 1
           for (int kr = 0; kr < 3 * KT; ++kr) {
-            const uint32_t bits = odd_at[kr * (D / 32) + t];
+            const uint32_t bits = odd_at[(kr / KT * KB + sub * KT + kr % KT) * (D / 32) + t];
             if (bits == 0 || k0 + kr % KT >= q.lim) continue;
             const float v = odd_value(kr / KT);
 #pragma unroll
@@ -382,7 +395,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
           }
       }
     }
-    if (k0 + KT < k_end) keep_voxel(b ^ 1);
+    if (kb + KB < k_end) keep_voxel(b ^ 1);
   }
 
   const float sum = l + __shfl_xor(l, 32);

@@ -334,3 +334,22 @@ def test_capped_scores_of_all_sizes(spread, dtype):
             u = ref.UNIT[dtype]  # float32 errors of the scores grow with them
             bound = mag * (2 * u + 4e-5 * max(1.0, spread)) + want.abs() * u + ref.TINY[dtype]
             assert bool(((got.double() - want).abs() <= bound).all()), f"cap {cap}"
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("d", [16, 32, 64])
+def test_voxels_over_tiles_that_end_anywhere(d, dtype):
+    """Keys that end inside a tile or between two, near voxels and far ones, hidden values that are not numbers."""
+    say(f"attention of voxels, {d} columns, {dtype}")
+    for n in (65, 127, 128, 129, 200, 319):
+        b = Batch([n, 70], [n, 333], 2, 2, d, dtype, seed=n)
+        b.check(f"{n} voxels", bias="voxel")
+        clean = b.run(causal=True, bias="voxel")
+        b.k_pos[n // 2:n] *= 4000  # too far for whole squares in float32
+        b.check(f"{n} voxels, some far", bias="voxel")
+        b.k_pos[n // 2:n] //= 4000
+        b.v[n - 1, :, ::3] = float("nan")  # the first document's last key, which only its last query sees
+        got = b.run(causal=True, bias="voxel")
+        seen = torch.ones(len(got), dtype=torch.bool, device=DEV)
+        seen[n - 1] = False
+        assert torch.equal(got[seen], clean[seen]) and bool(got[n - 1, :, ::3].isnan().all())
