@@ -165,9 +165,12 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
   int64_t splits, step;
   if (p.rows) {
     // Ranges of equal length until a launch has about 3072 workgroups (48 caches of up to 8192
-    // keys, 8 key heads: 209 us with one range, 168 to 160 with 5 to 16, 178 with 22), of 256 keys at least.
+    // keys, 8 key heads: 209 us with one range, 168 to 160 with 5 to 16, 178 with 22), of 256 keys at least, and
+    // of 128 while there are no more than eight (one token, 32 heads of 128: 1024 keys 10.4 us by
+    // four ranges, 9.2 by eight; 2048 by 16 even; 300 keys 6.7 by one, 7.7 by two).
     const int64_t work = std::max<int64_t>((int64_t)n_docs * kv_heads, 1);
-    splits = std::max<int64_t>(1, std::min<int64_t>((3072 + work - 1) / work, max_k / 256));
+    const int most = max_k < 512 ? 1 : std::max(max_k / 256, std::min(kFewRanges, max_k / 128));
+    splits = std::min<int64_t>((3072 + work - 1) / work, most);
     step = 128;
   } else {
     const int64_t tiles = n_q / kQueryTile + std::min<int64_t>(n_docs, n_q);
