@@ -70,7 +70,7 @@ struct Near {
 // from memory straight into the other half of LDS while one is multiplied.
 //
 // What bounds it: the vector and the matrix unit, each busy for 45 % of the cycles (documents of
-// up to 8192, 16 heads of 128, capped: 708 to 740 us, 0.94 PFLOP/s); with voxels and short rows
+// up to 8192, 16 heads of 128, capped: 700 to 730 us, 0.95 PFLOP/s); with voxels and short rows
 // the vector unit: a root, an exponential and eight more instructions a score (159 us).
 //
 // Workgroups with the same key head are neighbours in time on one XCD (workgroups go around
@@ -375,6 +375,9 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
       Frag fp[KT / 16];
 #pragma unroll
       for (int c = 0; c < KT / 16; ++c) fp[c] = to_frag<T>(s + 8 * c);
+      // all exponentials before the products: 712 -> 702 us where nothing else stands between them
+      // (other modes lose 1 to 6 %)
+      if constexpr (AHEAD && MODE == kCapped) __builtin_amdgcn_sched_barrier(0);
 
 #pragma unroll
       for (int c = 0; c < KT / 16; ++c)
