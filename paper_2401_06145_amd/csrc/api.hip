@@ -1121,6 +1121,31 @@ int check_attention(const spconv_attention_args* a) {
   return SPCONV_OK;
 }
 
+// cap tanh(u), u = scale s / cap, as s times a polynomial of u^2.  Up to a cap of 64 the polynomials
+// are the fits with the least largest error (of tanh: 1.3e-7 for |u| <= 1/2, and for |u| <= 0.11 by
+// two terms; for float32 rows 3.1e-9), which is 8e-6 of a score at most.  That error grows with
+// the cap: above 64 they are the series of tanh, taken where the first term left out is below
+// float32's resolution of the score (by two terms also where it is below 8e-6).
+void set_cap(AttnArgs* k, float cap, float scale, bool fine) {
+  static const double kFit[2][5] = {{0.9999976762, -0.333206552, 0.131451455, -0.04337247954, 0.0},
+                                    {0.9999999316, -0.3333277618, 0.1332057066, -0.05276212995, 0.01673756559}};
+  static const double kSeries[5] = {1.0, -1.0 / 3, 2.0 / 15, -17.0 / 315, 62.0 / 2835};
+  const bool fit = cap <= 64.0f;
+  // a cap near float32's least number: its scores are all but 0
+  const double by = std::min((double)scale / cap, 1e30), unit = scale * 1.4426950408889634;
+  k->cap = cap;
+  k->cap_log2 = (float)(cap * 1.4426950408889634);
+  k->cap_by = (float)by;
+  k->tanh_by = (float)(2 * 1.4426950408889634 * by);
+  for (int i = 0; i < 5; ++i) k->poly[i] = (float)((fit ? kFit[fine][i] : kSeries[i]) * unit);
+  k->poly_most = (float)std::min((fit ? 0.5 : fine ? 0.3 : 0.2) / by, 3e38);
+  // two terms take u^2's factor into their coefficient, which must stay far from float32's ends
+  const double low = fit ? 0.11 : std::max(0.026, std::pow(6e-5 / cap, 0.2));
+  k->low_most = by >= 1e-12 && by <= 1e12 ? (float)(low / by) : -1.0f;
+  k->low[0] = (float)((fit ? 0.99999394 : 1.0) * unit);
+  k->low[1] = (float)((fit ? -0.33132737 : -1.0 / 3) * unit * by * by);
+}
+
 AttnPlan plan_of(const spconv_attention_args* a) {
   return attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads, a->head_dim, a->dtype,
                         a->causal != 0);
@@ -1224,21 +1249,7 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   k.slopes = a->d_slopes, k.q_pos = a->d_q_pos, k.k_pos = a->d_k_pos;
   k.n_q = a->n_q, k.n_k = a->n_k, k.n_docs = a->n_docs, k.max_q = a->max_q, k.max_k = a->max_k;
   k.heads = a->heads, k.kv_heads = a->kv_heads, k.d = a->head_dim, k.causal = a->causal;
-  k.cap = a->cap;
-  k.cap_log2 = a->cap * kLog2e;
-  k.tanh_by = a->cap > 0.0f ? 2.0f * kLog2e * a->scale / a->cap : 0.0f;
-  // tanh(u) = u P(u^2) for |u| <= 1/2 (least largest error: 1.3e-7, for float32 rows 3.1e-9); the
-  // products' powers must stay far from float32's ends
-  const float by = a->cap > 0.0f ? a->scale / a->cap : 0.0f;
-  k.poly_most = by >= 1e-4f && by <= 1e4f ? 0.5f / by : -1.0f;
-  static const double kFit[2][5] = {{0.9999976762, -0.333206552, 0.131451455, -0.04337247954, 0.0},
-                                    {0.9999999316, -0.3333277618, 0.1332057066, -0.05276212995, 0.01673756559}};
-  // and with two terms for |u| <= 0.11, within 1.3e-7 too
-  k.low_most = k.poly_most * 0.22f;
-  k.low[0] = (float)(0.99999394 * k.cap_log2 * by);
-  k.low[1] = (float)(-0.33132737 * k.cap_log2 * std::pow((double)by, 3));
-  for (int i = 0; i < 5; ++i)
-    k.poly[i] = (float)(kFit[a->dtype == SPCONV_F32][i] * k.cap_log2 * std::pow((double)by, 2 * i + 1));
+  if (a->cap > 0.0f) set_cap(&k, a->cap, a->scale, a->dtype == SPCONV_F32);
   k.slope_by = a->cap > 0.0f ? kLog2e : 1.0f / a->scale;
   k.exp_by = a->cap > 0.0f ? 1.0f : a->scale * kLog2e;
   // below every finite score that matters, and finite in both units

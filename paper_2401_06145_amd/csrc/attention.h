@@ -26,9 +26,10 @@ struct AttnArgs {
   int n_docs, max_q, max_k, heads, kv_heads, d, causal;
   float cap;         // > 0: scores are capped
   float cap_log2;    // cap log2(e)
+  float cap_by;      // scale / cap
   float tanh_by;     // 2 log2(e) scale / cap
-  float low[2], low_most;    // capped scores of products up to low_most, the same with two terms (16-bit rows)
-  float poly[5], poly_most;  // capped scores of products up to poly_most, as an odd polynomial of them
+  float low[2], low_most;    // capped scores of products up to low_most, by two terms (16-bit rows)
+  float poly[5], poly_most;  // capped scores of products up to poly_most, as an odd polynomial
   float slope_by;    // from the slopes' units to the scores'
   float exp_by;      // from the scores' units to log2
   float floor;       // where the running maximum starts

@@ -185,15 +185,16 @@ struct Query {
 };
 
 // cap tanh(u), u = scale s / cap, in units of log2.  Where every product of the wave is small
-// (most are, as caps are meant for the few large ones) by an odd polynomial fitted to tanh
-// there: of degree 3 for |u| <= 0.11 and 7 for |u| <= 1/2, both within 1.3e-7 (FINE, for float32
-// rows: degree 9, 3e-9, as the error counts times the cap); else as tanh(u) =
-// 1 - 2 / (1 + e^{2u}), with its exact limits, within 1.2e-7.  3 or 5 instructions instead of 3
+// (most are, as caps are meant for the few large ones) as s times a polynomial of u^2, whose error
+// goes by the score and not by the cap (api.hip, set_cap): of degree 3 in u, 7, and 9 for float32
+// rows (FINE); else as tanh(u) = 1 - 2 / (1 + e^{2u}), with its exact limits, within 1.2e-7 of
+// the cap: a few of float32's steps, as such scores are at least a fifth of it.
+// 3 or 6 instructions instead of 3
 // and two transcendental ones, which take twice as long (whole documents, cap 50: 855 us, 767 with
 // degree 7, 719 to 735 with 3; a cap of 20, whose scores are not that small, is even).
 template <bool FINE>
 __device__ __forceinline__ float small_cap(const AttnArgs& a, float s) {
-  const float z = s * s;
+  const float u = s * a.cap_by, z = u * u;
   const float top = FINE ? fmaf(z, a.poly[4], a.poly[3]) : a.poly[3];
   return s * fmaf(fmaf(fmaf(z, top, a.poly[2]), z, a.poly[1]), z, a.poly[0]);
 }
