@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   const int doc = find_doc(a, slot, QT, &first);
   const Doc d = load_doc(a, doc);
   const int i0 = (slot - first) * QT;
-  if (i0 >= d.len_q) return;
+  if (i0 < 0 || i0 >= d.len_q) return;  // slots before the first document's are nobody's
   const int kvh = head / (a.heads / a.kv_heads);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = threadIdx.x % kWave, c32 = lane % 32, half = lane / 32;

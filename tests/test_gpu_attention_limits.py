@@ -30,3 +30,38 @@ def test_caps_of_all_sizes(cap, dtype):
                 bound = mag * (2 * u + 4e-5 * max(1.0, min(spread, cap))) + want.abs() * u + ref.TINY[dtype]
                 off = (got.double() - want).abs()
                 assert bool((off <= bound).all()), f"{bias}, scores of {spread}: {float((off / bound).max()):.2f} of the bound"
+
+
+SET_BEFORE = 7.0
+
+
+def run_into(b, q_start, k_start, max_q, max_k, causal=True):
+    """The C call on an output that is set before and a workspace of NaN: (output, bytes of workspace)."""
+    heads, kv, d, n, nk = b.q.shape[1], b.k.shape[1], b.q.shape[2], len(b.q), len(b.k)
+    out = torch.full_like(b.q, SET_BEFORE)
+    qs, ks = ints(q_start), ints(k_start)
+    a = B.AttentionArgs(d_q=b.q.data_ptr(), d_k=b.k.data_ptr(), d_v=b.v.data_ptr(), d_out=out.data_ptr(),
+                        q_row=heads * d, q_head=d, k_row=kv * d, k_head=d, v_row=kv * d, v_head=d, out_row=heads * d, out_head=d,
+                        d_q_start=qs.data_ptr(), d_k_start=ks.data_ptr(), n_q=n, n_k=nk, n_docs=len(q_start) - 1,
+                        max_q=max_q, max_k=max_k, heads=heads, kv_heads=kv, head_dim=d, dtype=B.DTYPES[b.q.dtype],
+                        causal=causal, scale=d ** -0.5)
+    need = B.spconv_attention_workspace_bytes(a)
+    workspace = torch.full((need // 4,), float("nan"), device=DEV).view(torch.uint8) if need else None
+    B.spconv_attention(a, workspace)
+    torch.cuda.synchronize()
+    return out, need
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_documents_from_the_middle_of_a_batch(dtype):
+    """A call on the documents from t on leaves the rows of those before as they are."""
+    say(f"attention on the last documents of a batch {dtype}")
+    for ql, kl, heads in (([300, 100, 70], [64, 60, 64], 2), ([127, 1, 200], [30, 64, 64], 1), ([5000, 64, 130], [9, 60, 64], 2)):
+        b = Batch(ql, kl, heads, heads, 32, dtype, seed=31)
+        want, mag = ref.attention(b.q, b.k, b.v, ql, kl, causal=True)
+        for t in (1, 2):
+            at = [sum(ql[:i]) for i in range(t, len(ql) + 1)]
+            got, need = run_into(b, at, [sum(kl[:i]) for i in range(t, len(kl) + 1)], max(ql[t:]), 64)
+            assert need == 0
+            assert bool((got[:at[0]] == SET_BEFORE).all()), f"rows before {at[0]}"
+            ref.check_attention(got[at[0]:], want[at[0]:], mag[at[0]:], f"documents from {t} on")
