@@ -341,7 +341,8 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
  *               with strides of rows and heads in elements, multiples of 16 bytes (a slice of
  *               a fused product will do); head_dim elements follow each other.
  *   max_q, max_k  at least the longest document's queries and keys: keys behind are not read,
- *               queries behind get no output.
+ *               queries behind get no output.  Their rows of d_out, and rows of no document
+ *               (before d_q_start[0], or from d_q_start[n_docs] on), stay as they are.
  * head_dim a multiple of 8 up to 256, 16-byte aligned pointers, rows of d_k and d_v at most
  * 32 MiB apart, max_k at most 2^30.  d_q_start must not descend.
  * Softmax statistics and sums are float32; the exponentials are rounded to `dtype` for the

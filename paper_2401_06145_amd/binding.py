@@ -530,7 +530,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.
 
     q [n_q][heads][d], k and v [n_k][kv_heads][d] may be slices of a fused product; q_start and
     k_start int32 [docs + 1]; k_len int32 [docs] where k and v are caches; scale defaults to
-    1 / sqrt(d).  Returns [n_q][heads][d]."""
+    1 / sqrt(d).  Returns [n_q][heads][d]; rows of no document and queries behind max_q are not set."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return attention(q, k, v, q_start, k_start, max_q, max_k, k_len, prefix, causal, scale, cap, slopes, q_pos, k_pos)

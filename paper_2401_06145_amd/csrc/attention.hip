@@ -16,6 +16,20 @@ namespace spc {
 namespace {
 using namespace attn;
 
+// Whether a row of the packed queries is a query that a document gives output: rows of no document
+// and queries behind max_q have no partial results, and their output stays as it is.  The
+// last document that starts at or before the row is the only one that can hold it.
+__device__ __forceinline__ bool has_output(const AttnArgs& a, int64_t row) {
+  int lo = 0;
+  for (int n = a.n_docs; n > 1;) {
+    const int half = n / 2;
+    if (a.q_start[lo + half] <= row) lo += half, n -= half;
+    else n = half;
+  }
+  const int64_t first = std::max(a.q_start[lo], 0);
+  return row >= first && row < a.q_start[lo + 1] && row - first < a.max_q;
+}
+
 // Joins the results of up to FEW key ranges: a group of G lanes per row and head, four columns a
 // lane; all maxima and sums are read together, then all outputs (11,003 rows of 8 heads of 32, three
 // ranges: 34 us with a wave per row and head, 11 so).
@@ -33,6 +47,7 @@ __global__ __launch_bounds__(256) void k_attn_join_few(AttnArgs a) {
     ml[s] = s < a.splits ? a.part_ml[(int64_t)s * rows + at] : f32x2{a.floor, 0.0f};
     top = fmaxf(top, ml[s][0]);
   }
+  if (!has_output(a, at / a.heads)) return;
   f32x4 p[kFewRanges];
 #pragma unroll
   for (int s = 0; s < kFewRanges; ++s) {
@@ -62,7 +77,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int64_t rows = a.n_q * a.heads;
   const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
   const int lane = threadIdx.x % kWave;
-  if (at >= rows) return;
+  if (at >= rows || !has_output(a, at / a.heads)) return;
   // the ranges' maxima and sums, one a lane
   float top = a.floor, sum = 0.0f;
   for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(int64_t)s * rows + at][0]);

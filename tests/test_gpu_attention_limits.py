@@ -65,3 +65,35 @@ def test_documents_from_the_middle_of_a_batch(dtype):
             assert need == 0
             assert bool((got[:at[0]] == SET_BEFORE).all()), f"rows before {at[0]}"
             ref.check_attention(got[at[0]:], want[at[0]:], mag[at[0]:], f"documents from {t} on")
+
+
+# queries and keys of each document, heads, key heads, width, whether the keys are split: few queries and many
+GAPS = [([4, 3, 2], [40, 30, 20], 8, 2, 64, False), ([4, 3, 2], [4000, 30, 900], 8, 2, 64, True),
+        ([1, 1, 1], [9000, 20, 12_000], 4, 1, 128, True), ([300, 100, 70], [64, 64, 64], 2, 2, 32, False),
+        ([300, 100, 70], [900, 100, 700], 2, 2, 32, True), ([130, 1, 200], [6000, 1, 3000], 1, 1, 256, True)]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("case", range(len(GAPS)))
+def test_rows_without_output_stay_as_they_are(case, dtype):
+    """Rows before the first document and behind the last (a batch padded to a fixed number of
+    rows), and queries behind max_q, whether the keys are split into ranges or not."""
+    ql, kl, heads, kv, d, split = GAPS[case]
+    say(f"attention with rows of no document, {ql} queries, {kl} keys, {d} columns, {dtype}")
+    before, behind = 5, 130
+    lens = [before, *ql, behind]
+    b = Batch(lens, [0, *kl, 0], heads, kv, d, dtype, seed=41)
+    at = [sum(lens[:i]) for i in range(1, len(lens))]
+    k_at = [sum(kl[:i]) for i in range(len(kl) + 1)]
+    want, mag = ref.attention(b.q, b.k, b.v, lens, [0, *kl, 0], causal=True)
+    for max_q in (max(ql), max(1, max(ql) - 1), max(1, max(ql) // 2)):
+        got, need = run_into(b, at, k_at, max_q, max(kl))
+        assert (need > 0) == split
+        has = torch.zeros(len(b.q), dtype=torch.bool, device=DEV)
+        for t, n in enumerate(ql):
+            has[at[t]:at[t] + min(n, max_q)] = True
+        assert bool((got[~has] == SET_BEFORE).all()), f"max_q {max_q}"
+        if max_q == max(ql):
+            ref.check_attention(got[has], want[has], mag[has], "the documents")
+        else:
+            assert bool(got[has].isfinite().all()) and not bool((got[has] == SET_BEFORE).all())
