@@ -1142,6 +1142,7 @@ void set_cap(AttnArgs* k, float cap, float scale, bool fine) {
   // two terms take u^2's factor into their coefficient, which must stay far from float32's ends
   const double low = fit ? 0.11 : std::max(0.026, std::pow(6e-5 / cap, 0.2));
   k->low_most = by >= 1e-12 && by <= 1e12 ? (float)(low / by) : -1.0f;
+  k->low_top = (float)(0.99999 * cap * 1.4426950408889634 * std::tanh(low));  // a rounding below
   k->low[0] = (float)((fit ? 0.99999394 : 1.0) * unit);
   k->low[1] = (float)((fit ? -0.33132737 : -1.0 / 3) * unit * by * by);
 }

@@ -29,6 +29,7 @@ struct AttnArgs {
   float cap_by;      // scale / cap
   float tanh_by;     // 2 log2(e) scale / cap
   float low[2], low_most;    // capped scores of products up to low_most, by two terms (16-bit rows)
+  float low_top;             // the score of low_most, in units of log2
   float poly[5], poly_most;  // capped scores of products up to poly_most, as an odd polynomial
   float slope_by;    // from the slopes' units to the scores'
   float exp_by;      // from the scores' units to log2

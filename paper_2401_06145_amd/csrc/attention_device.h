@@ -193,10 +193,14 @@ struct Query {
 // and two transcendental ones, which take twice as long (whole documents, cap 50: 855 us, 767 with
 // degree 7, 719 to 735 with 3; a cap of 20, whose scores are not that small, is even).
 template <bool FINE>
-__device__ __forceinline__ float small_cap(const AttnArgs& a, float s) {
+__device__ __forceinline__ float cap_factor(const AttnArgs& a, float s) {
   const float u = s * a.cap_by, z = u * u;
   const float top = FINE ? fmaf(z, a.poly[4], a.poly[3]) : a.poly[3];
-  return s * fmaf(fmaf(fmaf(z, top, a.poly[2]), z, a.poly[1]), z, a.poly[0]);
+  return fmaf(fmaf(fmaf(z, top, a.poly[2]), z, a.poly[1]), z, a.poly[0]);
+}
+__device__ __forceinline__ float cap_exactly(const AttnArgs& a, float s, float from) {
+  const float e = __builtin_amdgcn_exp2f(s * a.tanh_by);
+  return fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + e), from);
 }
 template <int COUNT, bool FINE>
 __device__ __forceinline__ void cap_scores(const AttnArgs& a, float* s) {
@@ -208,13 +212,26 @@ __device__ __forceinline__ void cap_scores(const AttnArgs& a, float* s) {
     for (int i = 0; i < COUNT; ++i) s[i] *= fmaf(s[i] * s[i], a.low[1], a.low[0]);
   } else if (!__any(most > a.poly_most)) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) s[i] = small_cap<FINE>(a, s[i]);
+    for (int i = 0; i < COUNT; ++i) s[i] *= cap_factor<FINE>(a, s[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-      const float e = __builtin_amdgcn_exp2f(s[i] * a.tanh_by);
-      s[i] = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + e), a.cap_log2);
-    }
+    for (int i = 0; i < COUNT; ++i) s[i] = cap_exactly(a, s[i], a.cap_log2);
+  }
+}
+// Capped scores less m, with what the caller knows of the wave's products: low, that none is beyond
+// low_most, and `most`, the largest magnitude of the lane's.
+template <int COUNT, bool FINE>
+__device__ __forceinline__ void cap_scores_less(const AttnArgs& a, float* s, bool low, float most, float m) {
+  if (!FINE && low) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i] = fmaf(s[i], fmaf(s[i] * s[i], a.low[1], a.low[0]), -m);
+  } else if (!__any(most > a.poly_most)) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i] = fmaf(s[i], cap_factor<FINE>(a, s[i]), -m);
+  } else {
+    const float from = a.cap_log2 - m;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i] = cap_exactly(a, s[i], from);
   }
 }
 

@@ -97,3 +97,47 @@ def test_rows_without_output_stay_as_they_are(case, dtype):
             ref.check_attention(got[has], want[has], mag[has], "the documents")
         else:
             assert bool(got[has].isfinite().all()) and not bool((got[has] == SET_BEFORE).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("cap", [20.0, 50.0, 60.0])
+@pytest.mark.parametrize("size", [1e-30, 1e-20, 1.0, 1e20, 1e33])
+def test_large_and_small_values_of_capped_keys(size, cap, dtype):
+    """Whatever the scores (all near -cap, all near +cap, small ones, one after the other), values
+    of every size keep it: exponentials are relative to the largest."""
+    if dtype == F16 and size != 1.0:
+        return  # float16 has no such values
+    say(f"attention with values of {size} under a cap of {cap} {dtype}")
+    for ql, kl, d in (([150, 40], [150, 333], 64), ([200], [700], 128), ([3, 1], [700, 90], 64)):
+        b = Batch(ql, kl, 4, 2, d, dtype, seed=51)
+        b.v = (b.v.float() * size).to(dtype)
+        towards = torch.randn(d, device=DEV)
+        for near in (1.0, -1.0, 0.0, 0.02):
+            # keys along one direction; queries along it, against it, small, or each differently
+            b.k = (torch.randn(b.k.shape, device=DEV) * 0.1 + towards).to(dtype)
+            q = torch.randn(b.q.shape, device=DEV) * 0.1 + (30 * near) * towards
+            if near == 0.02:
+                q *= torch.exp2(torch.randint(-3, 6, q.shape[:2], device=DEV).float())[..., None]
+            b.q = q.to(dtype)
+            got = b.run(causal=True, cap=cap)
+            want, mag = ref.attention(b.q, b.k, b.v, ql, kl, causal=True, cap=cap)
+            u = ref.UNIT[dtype]
+            # float32 errors of scores of up to the cap, products of up to some hundred behind them
+            bound = mag * (2 * u + 4e-5 * 30) + want.abs() * u + ref.TINY[dtype]
+            off = (got.double() - want).abs()
+            assert bool((off <= bound).all()), f"{near}: {float((off / bound).max()):.2f} of the bound"
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_infinite_products_under_a_cap(dtype):
+    """A product of -inf is a score of -cap, one of +inf a score of cap."""
+    say(f"attention with infinite products under a cap {dtype}")
+    for ql, kl, d in (([150, 40], [150, 333], 64), ([200], [700], 128), ([3, 1], [700, 90], 64)):
+        for first, last in ((0, 64), (0, 90), (10, 70), (40, 41)):
+            for sign in (-1.0, 1.0):
+                b = Batch(ql, kl, 4, 2, d, dtype, seed=61)
+                b.q = b.q.abs()
+                b.k[first:last] = sign * float("inf")
+                got = b.run(causal=True, cap=20.0)
+                want, mag = ref.attention(b.q, b.k, b.v, ql, kl, causal=True, cap=20.0)
+                ref.check_attention(got, want, mag, f"keys {first} to {last}, {sign}")
