@@ -6,7 +6,7 @@
 namespace spc {
 
 constexpr int kQueryTile = 128;  // queries of a workgroup of the many-query form
-// Strides of key and value rows, in bytes: a tile's rows are addressed with 32 bits.
+// Strides of key and value rows, in bytes: a tile's rows (up to 128) are addressed with 32 bits, unsigned.
 constexpr int64_t kMostRowBytes = 1 << 25;
 
 struct AttnArgs {

@@ -9,17 +9,19 @@ using namespace attn;
 // and no bias, in types of float32's exponents: a row whose scores are all within 0.11 of the cap
 // takes that bound for their maximum (exponentials of e^-13.2 at least), so that most tiles need
 // not look for it (whole documents 717 us; 4096 rows of 8 heads of 128 77 us, 93 with scores
-// beyond the bound, 83 and 92 by kAny, as measured in float16).  kVoxel: a bias by the distance of voxels, with or without a cap.  kAny:
-// everything else.
+// beyond the bound, 83 and 92 by kAny, as measured in float16).  kVoxel: a bias by the
+// distance of voxels, with or without a cap.  kAny: everything else.
 enum Mode { kBare, kCapped, kVoxel, kAny };
 constexpr float kMostBoundedCap = 60.0f;
 
 // 16 bytes a lane from memory straight into LDS, P times: those at `at[i]` of the `bytes` that
-// begin at `from` (zeros where they end before) to the wave's 1024 bytes at `to` + 4096 i.
+// begin at `from` (zeros where they end before, and at kNowhere) to the wave's 1024 bytes at
+// `to` + 4096 i.
 // Written as assembly because of the waits: of the builtin's loads the compiler awaits the
 // tile under way before it reads the tile that is there.  The caller waits (vmcnt) itself.
+constexpr uint32_t kNowhere = 0xfffffff0u;  // behind every buffer: 16 bytes from here on still have 32-bit offsets
 template <int P>
-__device__ __forceinline__ void bring_rows(const char* from, int bytes, char* to, const int* at) {
+__device__ __forceinline__ void bring_rows(const char* from, uint32_t bytes, char* to, const uint32_t* at) {
   const uint64_t base = reinterpret_cast<uint64_t>(from);
   const u32x4 rsrc = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base),
                       (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu),
@@ -145,17 +147,18 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   // out of the buffer's range, which gives zeros, as do rows behind the last key.
   const char* kp = static_cast<const char*>(a.k) + (d.k0 * a.k_row + (int64_t)kvh * a.k_head) * E;
   const char* vp = static_cast<const char*>(a.v) + (d.k0 * a.v_row + (int64_t)kvh * a.v_head) * E;
-  const int k_bytes = (int)a.k_row * E, v_bytes = (int)a.v_row * E;
-  int at_k[P], at_v[P];
+  const uint32_t k_bytes = (uint32_t)a.k_row * E, v_bytes = (uint32_t)a.v_row * E;
+  static_assert((KB - 1) * (uint64_t)kMostRowBytes + 256 * 4 <= kNowhere, "a tile's rows have offsets of 32 bits, unsigned");
+  uint32_t at_k[P], at_v[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const uint32_t p = (4 * i + wave) * kWave + lane, r = p / L::CH, c = p % L::CH;
     const int ck = L::k_chunk(r, c), cv = L::v_chunk(r, c);
-    at_k[i] = ck * (16 / E) < a.d ? r * k_bytes + 16 * ck : INT32_MIN;
-    at_v[i] = cv * (16 / E) < a.d ? r * v_bytes + 16 * cv : INT32_MIN;
+    at_k[i] = ck * (16 / E) < a.d ? r * k_bytes + 16 * ck : kNowhere;
+    at_v[i] = cv * (16 / E) < a.d ? r * v_bytes + 16 * cv : kNowhere;
   }
   const auto bring = [&](int k0, int b) {
-    const int rows = std::min(d.len_k - k0, KB);
+    const uint32_t rows = std::min(d.len_k - k0, KB);
     bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
     bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
   };

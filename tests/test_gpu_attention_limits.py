@@ -141,3 +141,22 @@ def test_infinite_products_under_a_cap(dtype):
                 got = b.run(causal=True, cap=20.0)
                 want, mag = ref.attention(b.q, b.k, b.v, ql, kl, causal=True, cap=20.0)
                 ref.check_attention(got, want, mag, f"keys {first} to {last}, {sign}")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("d,stride", [(8, 32 << 20), (24, 17 << 20), (24, 32 << 20), (40, 24 << 20), (64, 32 << 20)])
+def test_keys_far_apart(d, stride, dtype):
+    """Rows of keys and values up to 32 MiB apart, everything between them NaN: 128 of them span 4 GiB."""
+    say(f"attention with rows of {d} columns {stride} bytes apart {dtype}")
+    n, e = 140, torch.empty((), dtype=dtype).element_size()
+    b = Batch([n], [n], 2, 1, d, dtype, seed=71)
+    wide = torch.full((n, stride // e), float("nan"), device=DEV, dtype=dtype)
+    k, v = wide[:, :d].unflatten(1, (1, d)), wide[:, 2 * d:3 * d].unflatten(1, (1, d))
+    k.copy_(b.k), v.copy_(b.v)
+    s = ints([0, n])
+    for bias in ("none", "voxel"):
+        want, mag = ref.attention(b.q, b.k, b.v, [n], [n], **b.bias(bias))
+        ref.check_attention(B.attention(b.q, k, v, s, s, n, n, **b.bias(bias)), want, mag, bias)
+        few = torch.tensor([0, 5], dtype=torch.int32, device=DEV)
+        got = B.attention(b.q[:5], k, v, few, s, 5, n, **{**b.bias(bias), **({"q_pos": b.q_pos[:5]} if bias == "voxel" else {})})
+        ref.check_attention(got, want[:5], mag[:5], f"few queries, {bias}")
