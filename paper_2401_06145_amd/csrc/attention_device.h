@@ -136,6 +136,13 @@ __device__ __forceinline__ i16x4 read_columns(const char* p) {
       (__attribute__((address_space(3))) i16x4*)(__attribute__((address_space(3))) const void*)p);
 }
 
+// Exponentials are taken as 2^15 and less instead of 1 and less for float16 rows: rounded for the
+// product with V, those below 2^-25 of the largest would vanish from the sum of values, but
+// not from the sum of exponentials (131,072 keys at 2^-25.5 beside a dominant one hold 0.3 % of a
+// row).  The factor is part of both sums and leaves with their quotient.
+template <typename T>
+constexpr float kExpRaise = std::is_same_v<T, _Float16> ? 15.0f : 0.0f;
+
 // A document's part of the batch.
 struct Doc {
   int q0, len_q;

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
           for (int i = 0; i < 4; ++i) o[n][t][i] *= by;
         m[n] = top;
       }
-      const float off = m[n] * a.exp_by;
+      const float off = fmaf(m[n], a.exp_by, -kExpRaise<T>);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.exp_by, -off));

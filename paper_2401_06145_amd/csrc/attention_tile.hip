@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
             for (int i = 0; i < 16; ++i) o[t][i] *= by;
           m = top;
         }
-        const float off = m * a.exp_by;
+        const float off = fmaf(m, a.exp_by, -kExpRaise<T>);
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.exp_by, -off));
       }

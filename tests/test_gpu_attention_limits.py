@@ -160,3 +160,27 @@ def test_keys_far_apart(d, stride, dtype):
         few = torch.tensor([0, 5], dtype=torch.int32, device=DEV)
         got = B.attention(b.q[:5], k, v, few, s, 5, n, **{**b.bias(bias), **({"q_pos": b.q_pos[:5]} if bias == "voxel" else {})})
         ref.check_attention(got, want[:5], mag[:5], f"few queries, {bias}")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("below", [12.0, 25.6, 30.0])
+def test_many_weak_keys_beside_a_dominant_one(below, dtype):
+    """Keys whose weights are 2^-below of the largest keep their part of a long document's result."""
+    say(f"attention with weights of 2^-{below} {dtype}")
+    n, d, heads = 100_000, 64, 2
+    g = torch.Generator(DEV).manual_seed(81)
+    for ql in (1, 130):
+        q = torch.zeros((ql, heads, d), device=DEV)
+        k = torch.zeros((n, heads, d), device=DEV)
+        q[..., 0], k[..., 0] = 16.0, (32.0 - below * 0.6931472) / 2.0
+        k[n // 3, :, 0] = 16.0
+        k[..., 1] = torch.randn((n, heads), device=DEV, generator=g)  # not seen by the queries
+        v = 1.0 + 0.1 * torch.randn((n, heads, d), device=DEV, generator=g)
+        v[n // 3] = 0.0
+        q, k, v = q.to(dtype), k.to(dtype), v.to(dtype)
+        pos = torch.randint(0, 50, (n, 4), device=DEV, generator=g, dtype=torch.int32)
+        slopes = torch.full((heads,), 1e-6, device=DEV)
+        for bias in ({}, dict(slopes=slopes), dict(slopes=slopes, q_pos=pos[:ql], k_pos=pos)):
+            got = B.attention(q, k, v, ints([0, ql]), ints([0, n]), ql, n, **bias)
+            want, mag = ref.attention(q, k, v, [ql], [n], **bias)
+            ref.check_attention(got, want, mag, f"{ql} queries")
