@@ -193,13 +193,35 @@ __global__ __launch_bounds__(kThreads) void k_rms_norm_any(NormArgs a) {
   }
 }
 
+// Rows from `first` on, up to `most` of them.
+template <typename T, bool Q8>
+NormArgs part_of(const NormArgs& a, int64_t first, int64_t most) {
+  NormArgs p = a;
+  const auto at = [first](const void* from, int64_t ld, int64_t e) {
+    return from ? const_cast<char*>(static_cast<const char*>(from)) + first * ld * e : nullptr;
+  };
+  p.x = at(a.x, a.ld_x, sizeof(T));
+  p.res = at(a.res, a.ld_res, sizeof(T));
+  p.sum = at(a.sum, a.ld_sum, sizeof(T));
+  p.y = at(a.y, a.ld_y, Q8 ? 1 : sizeof(T));
+  p.scales = a.scales ? a.scales + first * a.ld_scales : nullptr;
+  p.n = std::min(a.n - first, most);
+  return p;
+}
+
 template <typename T, bool Q8>
 void norm_t(const NormArgs& a, bool wide, hipStream_t s) {
   const int chunks = (a.c + 7) / 8;
+  // more rows than one launch takes (2^31 work items, half of what it may have) go in parts
+  const auto launch = [&](auto kernel, int threads, int rows) {
+    const int64_t most = (int64_t)(0x7fffffff / threads) * rows;
+    for (int64_t first = 0; first < a.n; first += most) {
+      const NormArgs p = part_of<T, Q8>(a, first, most);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + rows - 1) / rows)), dim3(threads), 0, s, p);
+    }
+  };
   if (!wide || chunks > 2048) {
-#define SPC_N(G)                                                                                                  \
-  hipLaunchKernelGGL((k_rms_norm_any<T, Q8, G>), dim3((unsigned)((a.n + kThreads / G - 1) / (kThreads / G))), \
-                     dim3(kThreads), 0, s, a)
+#define SPC_N(G) launch(k_rms_norm_any<T, Q8, G>, kThreads, kThreads / G)
     // float16 with residual, by 16, 64 and 256 lanes a row: 24,914 x 4 5.4, 6.9, 13.4 us;
     // 20,000 x 129 8.8, 11.2, 19.2; 11,000 x 515 31.7, 17.9, 20.2; 11,000 x 1001 62.8, 34.0, 27.7
     if (!Q8 && a.c <= 192) SPC_N(16);
@@ -208,9 +230,7 @@ void norm_t(const NormArgs& a, bool wide, hipStream_t s) {
 #undef SPC_N
     return;
   }
-#define SPC_N(G, CH)                                                                                                 \
-  hipLaunchKernelGGL((k_rms_norm<T, Q8, G, CH>), dim3((unsigned)((a.n + threads_of(G) / G - 1) / (threads_of(G) / G))), \
-                     dim3(threads_of(G)), 0, s, a)
+#define SPC_N(G, CH) launch(k_rms_norm<T, Q8, G, CH>, threads_of(G), threads_of(G) / G)
   // One or two chunks a lane, so that a row's loads all fly at once and many rows fit a
   // CU: with a row of 4096 to a wave of 8 chunks a lane, 2000 rows in bfloat16 took 14.2 us
   // against 10.9 by a workgroup, 65,536 rows 339 against 303, 64 rows 8.9 against 3.8.

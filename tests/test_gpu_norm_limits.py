@@ -34,3 +34,25 @@ def test_8_bit_rows_of_a_sum(n, c, pad, shift, dtype):
     step = torch.maximum(want.abs() * 2.0 ** -4, ref.spread(scale, c) * 2.0 ** -10)
     off = (q.float().double() * ref.spread(scale, c) - want).abs()
     assert bool((off <= step * (1 + 2.0 ** -10) + want.abs() * slack + cancel).all())
+
+
+@pytest.mark.parametrize("c,residual,bits8", [(1032, False, False), (1040, False, True), (641, True, False)])
+def test_more_rows_than_one_launch_takes(c, residual, bits8):
+    """2^24 rows and more, each by a workgroup of 256 threads: 2^32 threads and more."""
+    say(f"norm of 16.8 million rows of {c}")
+    few, times = 4099, 4100  # a prime number of rows, again and again
+    assert few * times > 1 << 24
+    dtype = torch.float16
+    x, gamma = rows(few, c, dtype, 12).contiguous(), (1 + 0.2 * torch.randn(c, device=DEV)).to(dtype)
+    want = B.rms_norm(x, gamma, residual=x if residual else None, bits8=bits8)
+    wide = x.repeat(times, 1)
+    got = B.rms_norm(wide, gamma, residual=wide if residual else None, bits8=bits8)
+    for a, b in zip(got, want):
+        if b is None:
+            assert a is None
+            continue
+        a, b = (t.view(torch.uint8) if t.dtype == B.E4M3 else t for t in (a, b))
+        for part in a.view(times, few, -1).split(100):
+            assert bool((part == b).all())
+    del wide, got, a, part
+    torch.cuda.empty_cache()
