@@ -319,7 +319,8 @@ int spconv_rms_norm(const void* d_x, int64_t ld_x, const void* d_residual, int64
  * its group of eight, unless exact != 0: then, as for SPCONV_F32 and for few rows or outputs
  * always, they are summed in float32, at about half the speed.  k, ld_x and ld_w multiples of 16
  * (16-byte rows; SPCONV_EUNSUPPORTED otherwise), rows of d_x, d_w and d_x_scale at most 8 MiB
- * apart, d_x and d_w 16-byte aligned; any m and n.  k = 0 gives zeros.
+ * apart, d_x and d_w 16-byte aligned; any m and n up to what one launch takes (2^32 threads, 256
+ * for each 128 rows or fewer: SPCONV_EUNSUPPORTED beyond).  k = 0 gives zeros.
  * d_y must not overlap the inputs. */
 int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, int64_t ld_x_scale,
                          const void* d_w, int64_t ld_w, const float* d_w_scale, int64_t ld_w_scale, void* d_y,
@@ -344,7 +345,8 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
  *               queries behind get no output.  Their rows of d_out, and rows of no document
  *               (before d_q_start[0], or from d_q_start[n_docs] on), stay as they are.
  * head_dim a multiple of 8 up to 256, 16-byte aligned pointers, rows of d_k and d_v at most
- * 32 MiB apart, max_k at most 2^30.  d_q_start must not descend.
+ * 32 MiB apart, max_k at most 2^30, queries, heads and documents up to what one launch takes (2^32
+ * threads: SPCONV_EUNSUPPORTED beyond).  d_q_start must not descend.
  * Softmax statistics and sums are float32; the exponentials are rounded to `dtype` for the
  * product with V. */
 typedef struct {

@@ -1100,6 +1100,11 @@ int spconv_forward_noalloc(const spconv_map* m, const void* d_x, const void* d_w
 namespace {
 
 bool known_dtype(int dtype) { return dtype == SPCONV_F32 || dtype == SPCONV_F16 || dtype == SPCONV_BF16; }
+// A launcher's error as a status; hipErrorInvalidConfiguration is its refusal of the size.
+int launched(hipError_t e, const char* where) {
+  if (e == hipErrorInvalidConfiguration) return fail(SPCONV_EUNSUPPORTED, std::string(where) + ": more work than one launch takes");
+  return e == hipSuccess ? SPCONV_OK : hip_fail(e, where);
+}
 bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
 int check_attention(const spconv_attention_args* a) {
@@ -1210,10 +1215,9 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
   if (reinterpret_cast<uintptr_t>(d_y) % elem_bytes(dtype) != 0 || reinterpret_cast<uintptr_t>(d_x_scale) % 4 != 0 ||
       reinterpret_cast<uintptr_t>(d_w_scale) % 4 != 0)
     return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
-  SPC_TRY(launch_scaled_linear(d_x, ld_x, d_x_scale, ld_x_scale, d_w, ld_w, d_w_scale, ld_w_scale, d_y, ld_y, m, n, k,
-                               dtype, relu, exact != 0, static_cast<hipStream_t>(stream)),
-          "scaled product");
-  return SPCONV_OK;
+  return launched(launch_scaled_linear(d_x, ld_x, d_x_scale, ld_x_scale, d_w, ld_w, d_w_scale, ld_w_scale, d_y, ld_y, m, n,
+                                       k, dtype, relu, exact != 0, static_cast<hipStream_t>(stream)),
+                  "scaled product");
 }
 
 size_t spconv_attention_workspace_bytes(const spconv_attention_args* a) {
@@ -1256,8 +1260,7 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   // below every finite score that matters, and finite in both units
   k.floor = -3e38f / std::max(1.0f, k.exp_by);
   k.slots = (int)p.slots, k.splits = p.splits, k.chunk = p.chunk;
-  SPC_TRY(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention");
-  return SPCONV_OK;
+  return launched(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention");
 }
 
 // --------------------------------------------------------------- measurement

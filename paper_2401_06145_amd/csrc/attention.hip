@@ -174,8 +174,8 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
   const int group = heads / kv_heads;
   p.cols = (int64_t)max_q * group <= 64 ? max_q * group : 0;
   p.rows = p.cols > 0;
-  // the grid's third dimension holds the documents
-  if (p.rows && n_docs > 65535) p.rows = false;
+  // the grid's second dimension holds key heads and columns, the third the documents
+  if (p.rows && (n_docs > 65535 || (int64_t)kv_heads * ((p.cols + 15) / 16) > 65535)) p.rows = false;
   p.slots = n_q / kQueryTile + n_docs;
   int64_t splits, step;
   if (p.rows) {
@@ -198,6 +198,8 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
 }
 
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
+  // a row and head is joined by a wave at most
+  if (a.splits > 1 && !fits_launch(a.n_q * a.heads, kWave)) return hipErrorInvalidConfiguration;
   {
     ProfScope ps(KN_ATTENTION, s);
     const hipError_t e = p.rows ? launch_attention_rows(a, p, dtype, s) : launch_attention_tile(a, p, dtype, s);

@@ -490,7 +490,7 @@ void tile_t(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
-  if ((int64_t)a.heads * p.slots * p.splits > 0x7fffffff) return hipErrorInvalidValue;
+  if (!fits_launch((int64_t)a.heads * p.slots * p.splits, 256)) return hipErrorInvalidConfiguration;
   if (dtype == 0) tile_t<float>(a, s);
   else if (dtype == 1) tile_t<_Float16>(a, s);
   else tile_t<__bf16>(a, s);

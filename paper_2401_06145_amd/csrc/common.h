@@ -303,6 +303,10 @@ hipError_t launch_conv_small(const void* x, int64_t n_in, const void* w, const i
                              const void* residual, int relu, int64_t n_out, int c_in, int c_out, int dtype,
                              hipStream_t s);
 
+// A launch has fewer than 2^32 work items in each dimension, and up to 65535 workgroups in the
+// second and third.  Launchers return hipErrorInvalidConfiguration for more.
+inline bool fits_launch(int64_t workgroups, int threads) { return workgroups * threads <= 0xffffffffll; }
+
 // norm.hip: rows' root-mean-square norm with the residual's addition; y in the rows' type,
 // or e4m3 with a scale per 128 columns (bits8).  sum, residual: NULL or rows like x.
 hipError_t launch_rms_norm(const void* x, int64_t ld_x, const void* res, int64_t ld_res, const void* gamma, void* sum,

@@ -393,14 +393,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_rows(LinearArgs a) {
 // the whole (float32; the best tiles in brackets: 281 x 143 x 672 5.1 us [7.4], 1000 x 256 x 2048 9.0
 // [11.8], 70 x 4096 x 2048 9.9 [11.7], 281 x 1024 x 672 5.1 [6.5]; beyond it 1000 x 1024 x 512 6.4 [5.6],
 // 2500 x 256 x 640 8.4 [5.9]).
-bool few_rows(const LinearArgs& a) { return a.m <= 64 || (a.m + 63) / 64 * ((a.n + 31) / 32) <= 256; }
+bool few_rows(const LinearArgs& a) { return a.m <= 64 || (a.m + 63) / 64 * (((int64_t)a.n + 31) / 32) <= 256; }
 
 template <typename T>
-void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
-#define SPC_R(MT, NT, WAVES)                                                                                          \
-  hipLaunchKernelGGL((k_linear_rows<T, MT, NT, WAVES>),                                                               \
-                     dim3((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)((a.m + 16 * MT - 1) / (16 * MT))), \
-                     dim3(64 * WAVES), 0, s, a)
+hipError_t linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
+  const auto launch = [&](auto kernel, int64_t x, int64_t y, int threads) {
+    if (!fits_launch(x, threads) || y > 65535) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)x, (unsigned)y), dim3(threads), 0, s, a);
+    return hipGetLastError();
+  };
+  const int64_t n = a.n;
+#define SPC_R(MT, NT, WAVES) \
+  return launch(k_linear_rows<T, MT, NT, WAVES>, (n + 16 * NT - 1) / (16 * NT), (a.m + 16 * MT - 1) / (16 * MT), 64 * WAVES)
 // a wave for each block of columns, up to WAVES
 #define SPC_W(MT, NT, WAVES)              \
   do {                                    \
@@ -414,8 +418,8 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
     // fill the CUs twice, 32 of them a workgroup, as rows are then read half as often (64 x
     // 8192 x 4096: 29.6 -> 18.1 us), but for one strip of rows 16 and shorter workgroups (1 x 8192 x 8192:
     // 14.8 -> 13.6 us, with 32 outputs 19.7).
-    const auto fits = [&](int mt) { return (a.m + 16 * mt - 1) / (16 * mt) * ((a.n + 15) / 16) <= 256; };
-    const bool many = a.n > 4096;
+    const auto fits = [&](int mt) { return (a.m + 16 * mt - 1) / (16 * mt) * ((n + 15) / 16) <= 256; };
+    const bool many = n > 4096;
     if (many && a.m <= 16) SPC_W(1, 1, 8);
     else if (many && a.m <= 32) SPC_W(2, 2, 8);
     else if (many && a.m <= 48) SPC_W(3, 2, 8);
@@ -425,13 +429,11 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
     else if (a.m <= 48 || fits(3)) SPC_W(3, 1, 16);
     else if (a.m <= 64 || fits(4)) SPC_W(4, 1, 16);
     else SPC_W(4, 2, 8);
-    return;
   }
 #undef SPC_W
 #undef SPC_R
-#define SPC_T(EXACT, BM, BN, WM, WN, DEEP)                                                                            \
-  hipLaunchKernelGGL((k_linear_tile<T, EXACT, BM, BN, WM, WN, DEEP>),                                                 \
-                     dim3((unsigned)(((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN))), dim3(64 * WM * WN), 0, s, a)
+#define SPC_T(EXACT, BM, BN, WM, WN, DEEP) \
+  return launch(k_linear_tile<T, EXACT, BM, BN, WM, WN, DEEP>, (a.m + BM - 1) / BM * ((n + BN - 1) / BN), 1, 64 * WM * WN)
   // Tiles by how many of 128 x 128 there are.  Few leave CUs idle, for which smaller ones are
   // worth their reads (bfloat16, tiles of 64 x 64, 64 x 128, 128 x 128: 1500 x 2048 x 1024, 192 of
   // them: 8.3, 8.7, 9.9 us; 1000 x 1024 x 2048 9.1, 11.2, 14.9; 4000 x 1024 x 1024, 256 of them: 10.0, 8.8,
@@ -442,15 +444,14 @@ void linear_t(const LinearArgs& a, bool exact, hipStream_t s) {
   // with two blocks 9; 1024 columns: 14.9, and 13.6 with two).  Float32 outputs of such a tile do
   // not fit its one block; 64 x 128 does there (11,003 x 768 x 256: 11.6 against 15.6).  Else
   // large tiles where they fill the CUs.
-  const int64_t tiles = ((a.m + 127) / 128) * ((a.n + 127) / 128);
+  const int64_t tiles = ((a.m + 127) / 128) * ((n + 127) / 128);
   if constexpr (!std::is_same_v<T, float>) {
     if (!exact) {
       if (tiles <= 192) SPC_T(false, 64, 64, 2, 2, 2);
       else if (tiles <= 384) SPC_T(false, 64, 128, 2, 2, 2);
       else if (a.kb <= 4) SPC_T(false, 128, 128, 2, 2, 1);
-      else if (((a.m + 255) / 256) * ((a.n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4, 2);
+      else if (((a.m + 255) / 256) * ((n + 255) / 256) >= 256) SPC_T(false, 256, 256, 2, 4, 2);
       else SPC_T(false, 128, 128, 2, 2, 2);
-      return;
     }
   }
   if (tiles <= 192) SPC_T(true, 64, 64, 2, 2, 2);
@@ -465,17 +466,15 @@ hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, in
                                 const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
                                 int relu, bool exact, hipStream_t s) {
   if (m <= 0 || n <= 0) return hipSuccess;
-  if (((m + 63) / 64) * ((n + 63) / 64) > 0x7fffffff) return hipErrorInvalidValue;
   ProfScope ps(KN_SCALED_LINEAR, s);
   const int64_t e = dtype == 0 ? 4 : 2;
   LinearArgs a = {static_cast<const uint8_t*>(x), xs, static_cast<const uint8_t*>(w), ws, y, ld_x, ld_xs, ld_w, ld_ws,
                   ld_y, m, n, k, (k + kScaleBlock - 1) / kScaleBlock, relu, 0, 0};
   a.wide_xs = reinterpret_cast<uintptr_t>(xs) % 16 == 0 && ld_xs % 4 == 0;
   a.wide_y = reinterpret_cast<uintptr_t>(y) % 16 == 0 && ld_y * e % 16 == 0;
-  if (dtype == 0) linear_t<float>(a, true, s);
-  else if (dtype == 1) linear_t<_Float16>(a, exact, s);
-  else linear_t<__bf16>(a, exact, s);
-  return hipGetLastError();
+  if (dtype == 0) return linear_t<float>(a, true, s);
+  if (dtype == 1) return linear_t<_Float16>(a, exact, s);
+  return linear_t<__bf16>(a, exact, s);
 }
 
 }  // namespace spc

@@ -125,3 +125,24 @@ def test_binding_refuses_other_shapes():
                 dict(q=q.double())):
         with pytest.raises(ValueError):
             B.attention(**{"q": q, "k": q, "v": q, "q_start": at, "k_start": at, "max_q": 4, "max_k": 4, **bad})
+
+
+@pytest.mark.parametrize("kw", [
+    dict(m=(1 << 31) - 1, n=1, k=16), dict(m=(1 << 31) - 1, n=1, k=16, exact=1), dict(m=(1 << 31) - 1, n=1, k=16, dtype=0),
+    dict(m=1, n=(1 << 31) - 1, k=16), dict(m=40, n=(1 << 31) - 1, k=2048, ld_x=2048, ld_w=2048, ld_xs=16, ld_ws=16),
+    dict(m=(1 << 31) - 1, n=(1 << 31) - 1, k=16),
+])
+def test_product_of_more_than_one_launch_takes(kw):
+    """2^32 threads and more would start as fewer, without an error."""
+    assert linear(**{"ld_y": 1 << 31, **kw}) == B.SPCONV_EUNSUPPORTED
+    assert b"launch" in B.lib().spconv_last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n_q=(1 << 31) - 1, max_q=1 << 20, heads=128, kv_heads=2, q_row=8192, out_row=8192),
+    dict(n_q=70, n_docs=(1 << 31) - 1, max_q=40), dict(n_q=1 << 24, n_docs=1 << 24, max_q=40, heads=1, kv_heads=1, max_k=9),
+    dict(n_q=70, n_docs=1 << 28, max_q=1, heads=65535, kv_heads=65535, q_row=65535 * 64, out_row=65535 * 64),
+])
+def test_attention_of_more_than_one_launch_takes(kw):
+    assert B.lib().spconv_attention(ctypes.byref(attention_args(**kw)), P, 1 << 62, None) == B.SPCONV_EUNSUPPORTED
+    assert b"launch" in B.lib().spconv_last_error()
