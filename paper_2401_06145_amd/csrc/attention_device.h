@@ -186,7 +186,8 @@ __device__ __forceinline__ int find_doc(const AttnArgs& a, int slot, int tile, i
 // log2, the others in those of the products q.k (exp_by folds their scale into the
 // exponential's).  key(i) is the document's key of product i; hidden keys get -inf.
 struct Query {
-  float place, slope;  // place among the keys; slope in the scores' units
+  int place;           // among the keys
+  float slope;         // in the scores' units
   float x, y, z;       // voxel
   int lim;             // keys seen
 };
@@ -260,10 +261,11 @@ __device__ __forceinline__ void add_voxel_bias(const Query& q, float* s, Pos pos
     s[i] = fmaf(-q.slope, __builtin_amdgcn_sqrtf(fmaf(dx, dx, fmaf(dy, dy, dz * dz))), s[i]);
   }
 }
+// The difference of whole numbers: places from 2^24 on are not all float32 numbers, near distances are.
 template <int COUNT, typename Key>
 __device__ __forceinline__ void add_place_bias(const Query& q, float* s, Key key) {
 #pragma unroll
-  for (int i = 0; i < COUNT; ++i) s[i] = fmaf(-q.slope, fabsf(q.place - (float)key(i)), s[i]);
+  for (int i = 0; i < COUNT; ++i) s[i] = fmaf(-q.slope, fabsf((float)(q.place - key(i))), s[i]);
 }
 template <int COUNT, typename Key>
 __device__ __forceinline__ void hide(const Query& q, float* s, Key key) {
@@ -275,7 +277,7 @@ __device__ __forceinline__ void hide(const Query& q, float* s, Key key) {
 __device__ __forceinline__ Query make_query(const AttnArgs& a, const Doc& d, int i, int head, const int32_t* origin) {
   Query q;
   q.lim = seen(a, d, i);
-  q.place = (float)(d.len_k - d.len_q + i);
+  q.place = d.len_k - d.len_q + i;
   q.slope = a.slopes ? a.slopes[head] * a.slope_by : 0.0f;
   q.x = q.y = q.z = 0.0f;
   if (origin) {

@@ -184,3 +184,20 @@ def test_many_weak_keys_beside_a_dominant_one(below, dtype):
             got = B.attention(q, k, v, ints([0, ql]), ints([0, n]), ql, n, **bias)
             want, mag = ref.attention(q, k, v, [ql], [n], **bias)
             ref.check_attention(got, want, mag, f"{ql} queries")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_near_places_of_a_document_of_more_than_2_24_keys(dtype):
+    """Distances of one or two count, wherever in the document."""
+    n, d, tail = (1 << 24) + 1001, 8, 600
+    say(f"attention with a bias by place over {n} keys {dtype}")
+    g = torch.Generator(DEV).manual_seed(91)
+    k, v = (torch.zeros((n, 1, d), device=DEV, dtype=dtype) for _ in range(2))
+    k[-tail:], v[-tail:] = (torch.randn((tail, 1, d), device=DEV, generator=g).to(dtype) for _ in range(2))
+    slopes = torch.tensor([1.0], device=DEV)
+    for ql in (1, 5, 130):
+        q = torch.randn((ql, 1, d), device=DEV, generator=g).to(dtype)
+        got = B.attention(q, k, v, ints([0, ql]), ints([0, n]), ql, n, causal=True, slopes=slopes)
+        # keys 400 places and more before a query weigh e^-400
+        want, mag = ref.attention(q, k[-tail:].contiguous(), v[-tail:].contiguous(), [ql], [tail], causal=True, slopes=slopes)
+        ref.check_attention(got, want, mag, f"{ql} queries")
