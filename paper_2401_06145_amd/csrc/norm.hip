@@ -41,11 +41,11 @@ __device__ __forceinline__ float inverse_root(float m) {
 // An output.  One that becomes 8 bits keeps the first product's remainder, and its quotient by
 // the scale the quotient's: a value that a rounding carries over the middle between two e4m3
 // numbers is off by a whole step.  (6567 rows of 960 in bfloat16: 567 such values, so 546; of four
-// plain float32 operations 649.)
+// plain float32 operations 649.)  An infinite output has none.
 template <bool Q8>
 __device__ __forceinline__ float output(float v, float inv, float gamma) {
-  const float p = v * inv;
-  return Q8 ? fmaf(p, gamma, fmaf(v, inv, -p) * gamma) : p * gamma;
+  const float p = v * inv, y = p * gamma;
+  return Q8 && fabsf(y) < INFINITY ? fmaf(p, gamma, fmaf(v, inv, -p) * gamma) : y;
 }
 __device__ __forceinline__ float quotient(float y, float scale, float by) {
   const float q = y * by;

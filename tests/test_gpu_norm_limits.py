@@ -56,3 +56,24 @@ def test_more_rows_than_one_launch_takes(c, residual, bits8):
             assert bool((part == b).all())
     del wide, got, a, part
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("c,shift", [(256, 0), (1296, 0), (256, 1), (16400, 0)])
+def test_a_block_with_an_infinity(c, shift, dtype):
+    """A block with an infinite value has an infinite scale and stands for NaN; others are as without it."""
+    say(f"norm in 8 bits with an infinite gamma, {c} columns {dtype}")
+    x = rows(5, c, dtype, 13, 0, shift)
+    x[x == 0] = 1.0
+    gamma = (1 + 0.2 * torch.randn(c, device=DEV)).to(dtype)
+    want, want_scale, _ = B.rms_norm(x, gamma, bits8=True)
+    gamma[130] = float("inf")
+    q, scale, _ = B.rms_norm(x, gamma, bits8=True)
+    y = B.rms_norm(x, gamma)[0]
+    assert bool(y[:, 130].isinf().all())
+    hit = torch.zeros(c, dtype=torch.bool, device=DEV)
+    hit[128:256] = True
+    assert bool((scale[:, 1] == float("inf")).all()) and bool(q.float()[:, hit].isnan().all())
+    assert torch.equal(q.float()[:, ~hit], want.float()[:, ~hit])
+    keep = [i for i in range(scale.shape[1]) if i != 1]
+    assert torch.equal(scale[:, keep], want_scale[:, keep])
