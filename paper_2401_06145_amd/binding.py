@@ -461,7 +461,8 @@ def conv(in_coords: torch.Tensor, x: torch.Tensor, w: torch.Tensor, K: int, stri
 
 
 # ----------------------------------------------------------------------------
-# Transformer operators over features (rows are tokens)
+# Transformer operators over features (rows are tokens).  Forward only: tensors that require a
+# gradient are refused (ValueError) where gradients are recorded.
 # ----------------------------------------------------------------------------
 
 SCALE_BLOCK = 128  # columns of an 8-bit row (and rows of 8-bit weights) that share a scale

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
@@ -65,9 +66,13 @@ std::string shape(std::initializer_list<int64_t> v) {
 }
 
 bool tensor(PyObject* o) { return THPVariable_Check(o); }
+// A tensor whose derivatives nobody asks for: there are none to give.
 const at::Tensor& get(PyObject* o, const char* what) {
   if (!tensor(o)) throw Refused(std::string(what) + ": expected a tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if ((t.requires_grad() && at::GradMode::is_enabled()) || t._fw_grad(0).defined())
+    throw Refused(std::string(what) + ": requires a gradient, and this operator is forward only (use torch.no_grad() or detach())");
+  return t;
 }
 
 int dtype_of(at::ScalarType t, const char* what) {

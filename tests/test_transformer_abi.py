@@ -146,3 +146,28 @@ def test_product_of_more_than_one_launch_takes(kw):
 def test_attention_of_more_than_one_launch_takes(kw):
     assert B.lib().spconv_attention(ctypes.byref(attention_args(**kw)), P, 1 << 62, None) == B.SPCONV_EUNSUPPORTED
     assert b"launch" in B.lib().spconv_last_error()
+
+
+def test_binding_refuses_what_needs_gradients():
+    """Forward only: a call that autograd would have to record is refused, and is taken without it."""
+    x = torch.zeros((4, 32), dtype=torch.float16)
+    q = torch.zeros((4, 2, 32), dtype=torch.float16)
+    at, slopes = torch.tensor([0, 4], dtype=torch.int32), torch.ones(2)
+    q8, s = torch.zeros((4, 32), dtype=torch.uint8).view(B.E4M3), torch.ones((4, 1))
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    norm = lambda **kw: B.rms_norm(**{"x": x, "gamma": x[0], **kw})  # noqa: E731
+    linear = lambda **kw: B.scaled_linear(**{"x": q8, "x_scale": s, "w": q8, "w_scale": s[:1], "dtype": torch.float16, **kw})  # noqa: E731
+    attend = lambda **kw: B.attention(**{"q": q, "k": q, "v": q, "q_start": at, "k_start": at, "max_q": 4, "max_k": 4,  # noqa: E731
+                                         "slopes": slopes, **kw})
+    for call, kw in ((norm, dict(x=leaf(x))), (norm, dict(gamma=leaf(x[0]))), (norm, dict(residual=leaf(x) * 2)),
+                     (linear, dict(x_scale=leaf(s))), (linear, dict(w_scale=leaf(s[:1]))), (attend, dict(q=leaf(q))),
+                     (attend, dict(k=leaf(q))), (attend, dict(v=leaf(q))), (attend, dict(slopes=leaf(slopes)))):
+        with pytest.raises(ValueError, match="gradient"):
+            call(**kw)
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU|device"):  # taken, as far as this test's CPU tensors go
+            call(**kw)
+    import torch.autograd.forward_ad as fwd
+
+    with fwd.dual_level():
+        with pytest.raises(ValueError, match="gradient"):
+            norm(x=fwd.make_dual(x, torch.ones_like(x)))
