@@ -38,7 +38,10 @@ def _compile(src: str) -> str:
 
 def _torch_ops() -> str:
     """The binding against the installed torch (its folder is found without importing it)."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("the torch binding (_torch_ops.so) needs torch and its headers")
+    torch = os.path.dirname(spec.origin)
     tmp = TORCH_OPS + ".tmp"
     cmd = [HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__",
            "-I", INCLUDE, "-isystem", os.path.join(torch, "include"), "-isystem", "/opt/rocm/include",
@@ -52,18 +55,19 @@ def _torch_ops() -> str:
 
 
 def build(jobs: int = 8) -> str:
-    """Compile every HIP source for gfx950 and link libspconv.so, and the torch binding (always rebuilds)."""
+    """Compile every HIP source for gfx950 and link libspconv.so, and the torch binding (always rebuilds).
+    A binding that does not compile raises once the library, which needs no torch, is there."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=max(1, min(jobs, len(SOURCES)))) as ex:
         binding = ex.submit(_torch_ops)
         objs = list(ex.map(_compile, SOURCES))
-        binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    binding.result()
     return LIB
 
 
