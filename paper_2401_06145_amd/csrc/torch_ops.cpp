@@ -156,6 +156,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t count) {
   const at::Tensor& x = get(args[0], "x");
   if (x.dim() != 2) refuse("x", "rows", x);
   const int64_t n = x.size(0), c = x.size(1);
+  if (c > INT32_MAX) throw Refused("x: more than 2^31 - 1 columns");
   const at::ScalarType t = x.scalar_type();
   const int dtype = dtype_of(t, "x");
   const int64_t ld_x = rows(x, "x", t, n, c);

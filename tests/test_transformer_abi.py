@@ -171,3 +171,10 @@ def test_binding_refuses_what_needs_gradients():
     with fwd.dual_level():
         with pytest.raises(ValueError, match="gradient"):
             norm(x=fwd.make_dual(x, torch.ones_like(x)))
+
+
+def test_binding_refuses_rows_of_more_than_31_bits():
+    """Their number of columns must not wrap to a small one."""
+    x = torch.empty((1, (1 << 32) + 16), dtype=torch.float16)  # never touched
+    with pytest.raises(ValueError, match="columns"):
+        B.rms_norm(x, x[0])
