@@ -255,7 +255,7 @@ def spconv_concat_rows(a: torch.Tensor, b: torch.Tensor, out: torch.Tensor | Non
 def _ld(t: torch.Tensor) -> int:
     """Row stride; that of a single row is its length (torch's may be anything)."""
     n, c = t.shape
-    return t.stride(0) if n > 1 else max(t.stride(0), c)
+    return t.stride(0) if n > 1 else c
 
 
 def _device_stream(t: torch.Tensor, stream=None) -> int:

@@ -88,11 +88,19 @@ int dtype_of(at::ScalarType t, const char* what) {
 int64_t rows(const at::Tensor& t, const char* what, at::ScalarType dtype, int64_t n, int64_t c) {
   if (t.scalar_type() != dtype || t.dim() != 2 || t.size(0) != n || t.size(1) != c || (c > 1 && t.stride(1) != 1))
     refuse(what, std::string("rows ") + shape({n, c}) + " of " + c10::toString(dtype), t);
-  return n > 1 ? t.stride(0) : std::max(t.stride(0), c);
+  return n > 1 ? t.stride(0) : c;
 }
 void heads(const at::Tensor& t, const char* what, at::ScalarType dtype, int64_t d) {
   if (t.scalar_type() != dtype || t.dim() != 3 || t.size(2) != d || t.stride(2) != 1)
     refuse(what, "[rows][heads][" + std::to_string(d) + "] of " + c10::toString(dtype), t);
+}
+// Strides of rows and of heads; those of a single row or head are never used, and may be anything.
+struct Strides {
+  int64_t row, head;
+};
+Strides strides(const at::Tensor& t) {
+  const int64_t d = t.size(2);
+  return {t.size(0) > 1 ? t.stride(0) : t.size(1) * d, t.size(1) > 1 ? t.stride(1) : d};
 }
 template <typename T>
 const T* array(PyObject* o, const char* what, at::ScalarType dtype, std::initializer_list<int64_t> size, at::Device device) {
@@ -252,8 +260,9 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count) {
   const c10::OptionalDeviceGuard guard(q.device());
   at::Tensor out = empty(q.sizes(), t, q);
   a.d_q = q.data_ptr(), a.d_k = k.data_ptr(), a.d_v = v.data_ptr(), a.d_out = out.data_ptr();
-  a.q_row = q.stride(0), a.q_head = q.stride(1), a.k_row = k.stride(0), a.k_head = k.stride(1);
-  a.v_row = v.stride(0), a.v_head = v.stride(1), a.out_row = out.stride(0), a.out_head = out.stride(1);
+  const Strides sq = strides(q), sk = strides(k), sv = strides(v), so = strides(out);
+  a.q_row = sq.row, a.q_head = sq.head, a.k_row = sk.row, a.k_head = sk.head;
+  a.v_row = sv.row, a.v_head = sv.head, a.out_row = so.row, a.out_head = so.head;
   const size_t need = api.workspace(&a);
   at::Tensor workspace;
   if (need) workspace = empty({(int64_t)need}, at::kByte, q);
