@@ -45,3 +45,20 @@ def test_a_single_row_or_head_of_attention():
                   generator=g).to(torch.float16), k, v))
     want, mag = ref.attention(q1, k1, v1, [n], [n], causal=True)
     ref.check_attention(B.attention(q1, k1, v1, ints([0, n]), ints([0, n]), n, n, causal=True), want, mag, "one head")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", [(300, 700, 640), (300, 700, 128), (2100, 700, 272), (3333, 1203, 656), (4352, 4096, 1152), (4097, 4200, 1408)])
+def test_scales_that_end_inside_16_bytes(m, n, k, dtype):
+    """Row scales 4 a load, of rows that end inside one: what lies behind a row's last scale is never used."""
+    say(f"scaled product with padded row scales {m} x {n} x {k} {dtype}")
+    kb = -(-k // 128)
+    x, w, ws = bits8(m, k, 61), bits8(n, k, 62), scales(-(-n // 128), k, 64) * 1e-4
+    wide = torch.full((m, -(-kb // 4) * 4), float("nan"), device=DEV)
+    wide[:, :kb] = scales(m, k, 63) * 1e-4
+    xs = wide[:, :kb]
+    assert xs.stride(0) % 4 == 0 and kb % 4 != 0
+    want, mag = ref.scaled_linear(x, xs, w, ws)
+    ref.check_linear(B.scaled_linear(x, xs, w, ws, dtype, exact=True), want, mag, k, "padded scales")
+    # as scales without gaps, loaded one by one
+    assert torch.equal(B.scaled_linear(x, xs, w, ws, dtype), B.scaled_linear(x, xs.contiguous(), w, ws, dtype))
