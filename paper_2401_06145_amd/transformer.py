@@ -36,6 +36,7 @@ class Config:
     inner: int = 1024
     cap: float = 30.0     # of the scores; 0: none
     eps: float = 1e-6
+    exact: bool = False   # products summed in float32 throughout (spconv_scaled_linear's exact), at about half the rate
 
     @property
     def head_dim(self) -> int:
@@ -85,7 +86,7 @@ class Transformer:
         self.slopes = torch.exp2(-8.0 * torch.arange(1, c.heads + 1) / c.heads).to(self.device)
 
     def _linear(self, rows, weight, relu=False):
-        return B.scaled_linear(rows[0], rows[1], weight[0], weight[1], self.dtype, relu=relu)
+        return B.scaled_linear(rows[0], rows[1], weight[0], weight[1], self.dtype, relu=relu, exact=self.config.exact)
 
     def _run(self, x: torch.Tensor, attend) -> torch.Tensor:
         """The layers on rows x; attend(layer, q, k, v) is their attention."""

@@ -178,3 +178,14 @@ def test_binding_refuses_rows_of_more_than_31_bits():
     x = torch.empty((1, (1 << 32) + 16), dtype=torch.float16)  # never touched
     with pytest.raises(ValueError, match="columns"):
         B.rms_norm(x, x[0])
+
+
+@pytest.mark.parametrize("exact", [False, True])
+def test_transformer_asks_for_exact_products(exact, monkeypatch):
+    from paper_2401_06145_amd import transformer
+
+    asked = []
+    monkeypatch.setattr(B, "scaled_linear", lambda *a, **kw: asked.append(kw["exact"]))
+    model = transformer.Transformer(transformer.Config(width=32, heads=2, kv_heads=1, layers=1, inner=32, exact=exact), device="cpu")
+    model._linear((None, None), model.layers[0]["qkv"])
+    assert asked == [exact]
