@@ -278,7 +278,11 @@ __device__ __forceinline__ Query make_query(const AttnArgs& a, const Doc& d, int
   Query q;
   q.lim = seen(a, d, i);
   q.place = d.len_k - d.len_q + i;
-  q.slope = a.slopes ? a.slopes[head] * a.slope_by : 0.0f;
+  q.slope = 0.0f;
+  if (a.slopes) {  // a finite one stays finite in the scores' units: infinity times the distance 0 is not a number
+    const float given = a.slopes[head], there = given * a.slope_by;
+    q.slope = fabsf(given) < INFINITY ? fminf(fmaxf(there, -3e38f), 3e38f) : there;
+  }
   q.x = q.y = q.z = 0.0f;
   if (origin) {
     const Voxel v = voxel_from(a.q_pos + 4 * (int64_t)(d.q0 + i), origin);

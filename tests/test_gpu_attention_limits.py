@@ -201,3 +201,18 @@ def test_near_places_of_a_document_of_more_than_2_24_keys(dtype):
         # keys 400 places and more before a query weigh e^-400
         want, mag = ref.attention(q, k[-tail:].contiguous(), v[-tail:].contiguous(), [ql], [tail], causal=True, slopes=slopes)
         ref.check_attention(got, want, mag, f"{ql} queries")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_slopes_up_to_the_largest_number(dtype):
+    """A slope of float32's largest number leaves the key at distance 0 alone."""
+    say(f"attention with the steepest slopes {dtype}")
+    for ql, d in (([150], 64), ([3], 128)):
+        b = Batch(ql, ql, 2, 2, d, dtype, seed=101)
+        b.k_pos = b.q_pos = torch.arange(ql[0] * 4, device=DEV, dtype=torch.int32).view(-1, 4)
+        slopes = torch.tensor([3.4028234e38, 1e38], device=DEV)
+        for bias in (dict(slopes=slopes), dict(slopes=slopes, q_pos=b.q_pos, k_pos=b.k_pos)):
+            for cap in (0.0, 20.0):
+                want, mag = ref.attention(b.q, b.k, b.v, ql, ql, causal=True, cap=cap, **bias)
+                assert torch.equal(want, b.v.double())
+                ref.check_attention(b.run(causal=True, cap=cap, bias="none", **bias), want, mag, "steepest slopes")
