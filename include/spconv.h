@@ -335,7 +335,8 @@ int spconv_scaled_linear(const void* d_x, int64_t ld_x, const float* d_x_scale, 
  *     s_j = cap tanh(scale q.k_j / cap)   (cap > 0; else scale q.k_j)   - slope dist(i, j)
  *     out = sum_j softmax(s)_j v_j        over the keys it sees
  * with dist = |p - j|, or the Euclidean distance of the two voxels where positions are given
- * (rows (b, x, y, z) as the layers' coordinates; b is not used).  A query that sees no key, or
+ * (rows (b, x, y, z) as the layers' coordinates; b is not used; coordinates are float32 as seen from
+ * one of the document's queries, exact up to 2^24 from it).  A query that sees no key, or
  * none with a score above -inf, gets zeros.  Hidden keys' values may be anything, NaN included.
  * Query head h reads key head h / (heads / kv_heads).
  *   d_q, d_out  rows n_q, heads, head_dim; d_k, d_v: rows n_k, kv_heads, head_dim, all in `dtype`,

@@ -9,7 +9,9 @@
 // float32 registers beside the unnormalised output, which is rescaled when the maximum
 // grows.  Scores are computed transposed, S^T = K Q^T: a lane then holds scores of one query
 // only, and its exponentials are, as they lie, the second operand of out^T = V^T P^T.
-// P is rounded to the rows' type for that product (sums of P are not).
+// P is rounded to the rows' type for that product, which is what the matrix unit multiplies at full
+// rate; sums of P are not.  The rounding is at most that of the result once more (bfloat16: 0.0019
+// to 0.0023 of the result in place of 0.0017, float16 and float32 even).
 #include "attention_device.h"
 
 namespace spc {

@@ -13,7 +13,7 @@ using namespace attn;
 // ---------------------------------------------------------------------------
 //
 // What bounds it: memory.  48 caches of up to 8192 keys (8 key heads of 128, 16 bits, 801 MB) take
-// 156 to 160 us, 5.0 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
+// 155 to 160 us, 5.0 TB/s, what a large copy reaches; two workgroups a CU keep enough loads under
 // way (one: 183 us), except for rows of more than 256 bytes, whose registers would spill.
 // 32 and 64 columns a workgroup only where their sums fit its registers, else more workgroups
 // for a key head's columns (two documents of 49, 8 heads of 96, float32: 9.5 us, with 64 columns a

@@ -73,9 +73,10 @@ struct Near {
 // keys at a time through LDS; each wave has 32 of the queries.  The next tile of K and V is on its way
 // from memory straight into the other half of LDS while one is multiplied.
 //
-// What bounds it: the vector and the matrix unit, each busy for 45 % of the cycles (documents of
-// up to 8192, 16 heads of 128, capped: 700 to 730 us, 0.95 PFLOP/s); with voxels and short rows
-// the vector unit: a root, an exponential and eight more instructions a score (159 us).
+// What bounds it: the vector and the matrix unit, busy for 52 and 44 % of the cycles (documents of
+// up to 8192, 16 heads of 128, capped: 711 to 775 us by the machine, 0.9 to 0.96 PFLOP/s); with voxels
+// and short rows the vector unit, 62 %: a root, an exponential and eight more instructions a
+// score and head (160 us).
 //
 // Workgroups with the same key head are neighbours in time on one XCD (workgroups go around
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,

@@ -6,8 +6,8 @@
 // A row is read once and stays in registers, in float32, between the sum of squares and
 // the output; the norm is that of the unrounded sum.  What bounds it is memory: 16-bit
 // rows with a residual move 7 bytes an element (x, residual, sum, q).  65,536 x 4096 in
-// bfloat16, 1.88 GB: 303 us, 6.2 TB/s (stores through the caches cost 3 %); 11,003 x 256
-// in float16 5.9 us; one token of 1024 2.9 us, of which starting the kernel is most.
+// bfloat16, 1.89 GB: 305 us, 6.2 TB/s (stores through the caches cost 3 %); 11,003 x 256
+// in float16 5.7 us; one token of 1024 2.2 us, of which starting the kernel is most.
 #include <algorithm>
 #include <type_traits>
 
