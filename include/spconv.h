@@ -17,7 +17,8 @@
  *
  * Next to the layers stand the operators of a transformer over their features (voxels as
  * tokens, a batch's scenes as documents): spconv_rms_norm, spconv_scaled_linear and
- * spconv_attention.
+ * spconv_attention; and, to serve documents token by token or in chunks, spconv_rotate_heads and
+ * a cache of pages: spconv_cache_write, spconv_cache_read and spconv_cached_attention.
  *
  * Conventions shared by every entry point:
  *   - Pointers named d_* are DEVICE pointers, h_* HOST pointers.  The caller owns
@@ -377,13 +378,91 @@ typedef struct {
 size_t spconv_attention_workspace_bytes(const spconv_attention_args* args);
 int spconv_attention(const spconv_attention_args* args, void* d_workspace, size_t ws_bytes, void* stream);
 
+/* Queries and keys before attention: the root-mean-square norm of each head (where a gamma is
+ * given), and the rotation of its first `rotated` columns by the row's position:
+ *     y = x / sqrt(mean(x^2) + eps) * gamma                       (or y = x)
+ *     pair (a, b) number j turns by p f_j:  gain (a cos - b sin),  gain (a sin + b cos)
+ * Pair j is columns (j, j + rotated / 2), or (2 j, 2 j + 1) where interleaved != 0; columns from
+ * `rotated` on stay y.  p is d_pos[row], or, with voxels != 0, the coordinate 1 + j % 3 of the
+ * voxel d_pos[row] = (b, x, y, z).  Positions may be negative.  d_freq holds f_j in radians a
+ * position, in float64, as are the angles: far places keep their accuracy.  Frequencies and gain
+ * scaled for contexts longer than trained on are the caller's.
+ *   d_q, d_k    rows n, heads (kv_heads), head_dim in `dtype`; kv_heads 0: no keys.  Strides in
+ *               elements, any; 16- or 8-byte accesses where they and the columns allow them.
+ *   d_q_out, d_k_out  the same shapes; may be d_q and d_k with the same strides, and overlap them
+ *               in no other way.
+ *   d_q_gamma, d_k_gamma  [head_dim] in `dtype`, each NULL for no norm.
+ * head_dim 1 to 256, rotated even and at most head_dim (0: the norm alone; d_pos and d_freq unused). */
+typedef struct {
+  const void* d_q;
+  void* d_q_out;
+  const void* d_k;
+  void* d_k_out;
+  int64_t q_row, q_head, q_out_row, q_out_head, k_row, k_head, k_out_row, k_out_head; /* strides in elements */
+  const void* d_q_gamma;
+  const void* d_k_gamma;
+  const int32_t* d_pos; /* [n], or [n][4] */
+  const double* d_freq; /* [rotated / 2] */
+  int64_t n;
+  int heads, kv_heads, head_dim, rotated;
+  int dtype, interleaved, voxels;
+  float eps, gain;
+} spconv_rotation;
+int spconv_rotate_heads(const spconv_rotation* args, void* stream);
+
+/* A cache of pages.  A page holds `page` keys' and values' rows of all heads, [kv_heads][page]
+ * [head_dim] each; document t's key j is row j % page of page table[t][j / page].  Documents may
+ * share pages.  Where scales are given, pages are e4m3 bytes: a row of one head is q * scale,
+ * scale = max(max|x| / 448, 2^-126), q = x / scale rounded to nearest even (NaN stays NaN; a row
+ * with an infinity gets an infinite scale and stands for NaN; scales that the caller writes are
+ * at least 2^-126).  Else they hold rows of the calls' `dtype`.
+ * page is a power of two up to 65536, head_dim a multiple of 8 (8 bits: of 16) up to 256, pages
+ * 16-byte aligned, table_row * page at most 2^30.  Entries of the table that no key of a call
+ * needs are not read; one outside [0, n_pages) is never followed: nothing is written there, and its
+ * keys and values are zeros. */
+typedef struct {
+  void* d_k; /* [n_pages][kv_heads][page][head_dim] */
+  void* d_v;
+  float* d_k_scale; /* [n_pages][kv_heads][page], or both NULL */
+  float* d_v_scale;
+  const int32_t* d_table; /* [n_docs][table_row] */
+  int64_t n_pages;
+  int n_docs, table_row, page, kv_heads, head_dim;
+} spconv_pages;
+
+/* New tokens' keys and values into their documents' pages.  Row q_start[t] + i is new token i of
+ * document t, which holds k_len[t] keys with the new ones: as spconv_cached_attention's queries,
+ * it goes to place k_len[t] - (q_start[t + 1] - q_start[t]) + i.  Rows of no document, and places
+ * before 0 or behind the table, are left out.  d_k, d_v: rows n, kv_heads, head_dim in `dtype`, 16-byte
+ * aligned, strides multiples of 16 bytes.  Two rows for one place (documents that share a page)
+ * leave either's elements. */
+int spconv_cache_write(const spconv_pages* pages, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
+                       int64_t v_row, int64_t v_head, const int32_t* d_q_start, const int32_t* d_k_len, int64_t n,
+                       int dtype, void* stream);
+
+/* Documents' first keys and values, in `dtype`: row start[t] + i of d_k and d_v gets those of key i
+ * of document t, for start[t + 1] - start[t] keys.  Rows of no document stay as they are; keys
+ * behind the table are zeros.  Strides as spconv_cache_write's. */
+int spconv_cache_read(const spconv_pages* pages, void* d_k, int64_t k_row, int64_t k_head, void* d_v, int64_t v_row,
+                      int64_t v_head, const int32_t* d_start, int64_t n, int dtype, void* stream);
+
+/* spconv_attention over pages: document t's keys are its k_len[t] (at most table_row * page) in
+ * the pages, its queries the new tokens (one, or a chunk), whose keys are among them.  Of `args`
+ * d_k, d_v, their strides, d_k_start and n_k are not used, d_k_len has to be given, and voxels are
+ * not supported; n_docs, kv_heads and head_dim are those of the pages.  The rest is as there: its
+ * masks, prefix, cap, bias by place, rows that stay as they are, and limits.  8-bit rows count as
+ * the exact values that they stand for, except in float16 where those are subnormal. */
+size_t spconv_cached_attention_workspace_bytes(const spconv_pages* pages, const spconv_attention_args* args);
+int spconv_cached_attention(const spconv_pages* pages, const spconv_attention_args* args, void* d_workspace,
+                            size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------ measurement --
  * Event timing: for every id whose bit is set in `mask`, the library records HIP
  * events on the caller's stream around that phase of spconv_build_map /
  * spconv_forward (ids 0..10: bounds, sort, outcoords, backward, balance, forward,
  * readback, metadata (the table fill of maps other than odd-K submanifold ones),
  * gather, gemm, scatter) or around each launch of that kernel
- * (ids 16..39; spconv_profile_phase_name() gives the names, "" for unused ids).
+ * (ids 16..42; spconv_profile_phase_name() gives the names, "" for unused ids).
  * mask = 0 turns timing off.  spconv_profile_read() waits for the recorded events
  * and writes the summed milliseconds and the number of timed intervals per id
  * into host arrays of at least spconv_profile_phase_count() entries; reset != 0

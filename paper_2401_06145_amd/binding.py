@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import os
+from dataclasses import dataclass
 
 import torch
 
@@ -31,7 +33,8 @@ EXPORTED = [
     "spconv_map_pairs", "spconv_map_copy_pairs", "spconv_map_copy_out_coords", "spconv_free_map",
     "spconv_forward_workspace_bytes", "spconv_forward", "spconv_forward_ex", "spconv_forward_noalloc",
     "spconv_concat_rows", "spconv_rms_norm", "spconv_scaled_linear", "spconv_attention",
-    "spconv_attention_workspace_bytes",
+    "spconv_attention_workspace_bytes", "spconv_rotate_heads", "spconv_cache_write", "spconv_cache_read",
+    "spconv_cached_attention", "spconv_cached_attention_workspace_bytes",
     "spconv_forward_plan", "spconv_profile_enable", "spconv_profile_phase_count",
     "spconv_profile_phase_name", "spconv_profile_read", "spconv_last_error",
 ]
@@ -76,6 +79,22 @@ class AttentionArgs(ctypes.Structure):
                 + [(n, ctypes.c_int) for n in ("n_docs", "max_q", "max_k", "heads", "kv_heads", "head_dim", "dtype",
                                                "causal")]
                 + [("scale", ctypes.c_float), ("cap", ctypes.c_float)])
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("d_q", "d_q_out", "d_k", "d_k_out")]
+                + [(n, ctypes.c_int64) for n in ("q_row", "q_head", "q_out_row", "q_out_head", "k_row", "k_head", "k_out_row",
+                                                 "k_out_head")]
+                + [(n, ctypes.c_void_p) for n in ("d_q_gamma", "d_k_gamma", "d_pos", "d_freq")]
+                + [("n", ctypes.c_int64)]
+                + [(n, ctypes.c_int) for n in ("heads", "kv_heads", "head_dim", "rotated", "dtype", "interleaved", "voxels")]
+                + [("eps", ctypes.c_float), ("gain", ctypes.c_float)])
+
+
+class PagesArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("d_k", "d_v", "d_k_scale", "d_v_scale", "d_table")]
+                + [("n_pages", ctypes.c_int64)]
+                + [(n, ctypes.c_int) for n in ("n_docs", "table_row", "page", "kv_heads", "head_dim")])
 
 
 _lib = None
@@ -134,6 +153,17 @@ def lib() -> ctypes.CDLL:
     L.spconv_attention_workspace_bytes.restype = sz
     L.spconv_attention.argtypes = [ctypes.POINTER(AttentionArgs), vp, sz, vp]
     L.spconv_attention.restype = c_int
+    pages, attn = ctypes.POINTER(PagesArgs), ctypes.POINTER(AttentionArgs)
+    L.spconv_rotate_heads.argtypes = [ctypes.POINTER(Rotation), vp]
+    L.spconv_rotate_heads.restype = c_int
+    L.spconv_cache_write.argtypes = [pages, vp, i64, i64, vp, i64, i64, vp, vp, i64, c_int, vp]
+    L.spconv_cache_write.restype = c_int
+    L.spconv_cache_read.argtypes = [pages, vp, i64, i64, vp, i64, i64, vp, i64, c_int, vp]
+    L.spconv_cache_read.restype = c_int
+    L.spconv_cached_attention_workspace_bytes.argtypes = [pages, attn]
+    L.spconv_cached_attention_workspace_bytes.restype = sz
+    L.spconv_cached_attention.argtypes = [pages, attn, vp, sz, vp]
+    L.spconv_cached_attention.restype = c_int
     L.spconv_forward_plan.argtypes = [vp, c_int, c_int, c_int, optp, ctypes.POINTER(PlanInfo)]
     L.spconv_forward_plan.restype = c_int
     L.spconv_profile_enable.argtypes = [ctypes.c_uint64]
@@ -298,6 +328,41 @@ def spconv_attention(args: AttentionArgs, workspace: torch.Tensor | None, stream
     st = lib().spconv_attention(ctypes.byref(args), ws, n, stream)
     if st:
         _check(st, "spconv_attention")
+
+
+def _handle(stream) -> int:
+    """A stream's handle; by default the current device's current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def spconv_rotate_heads(args: Rotation, stream=None) -> None:
+    _check(lib().spconv_rotate_heads(ctypes.byref(args), _handle(stream)), "spconv_rotate_heads")
+
+
+def spconv_cache_write(pages: PagesArgs, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, k_len: torch.Tensor,
+                       stream=None) -> None:
+    st = lib().spconv_cache_write(ctypes.byref(pages), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                  v.stride(1), q_start.data_ptr(), k_len.data_ptr(), k.shape[0], DTYPES[k.dtype],
+                                  _device_stream(k, stream))
+    _check(st, "spconv_cache_write")
+
+
+def spconv_cache_read(pages: PagesArgs, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, stream=None) -> None:
+    st = lib().spconv_cache_read(ctypes.byref(pages), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                 v.stride(1), start.data_ptr(), k.shape[0], DTYPES[k.dtype], _device_stream(k, stream))
+    _check(st, "spconv_cache_read")
+
+
+def spconv_cached_attention_workspace_bytes(pages: PagesArgs, args: AttentionArgs) -> int:
+    return int(lib().spconv_cached_attention_workspace_bytes(ctypes.byref(pages), ctypes.byref(args)))
+
+
+def spconv_cached_attention(pages: PagesArgs, args: AttentionArgs, workspace: torch.Tensor | None, stream=None) -> None:
+    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    st = lib().spconv_cached_attention(ctypes.byref(pages), ctypes.byref(args), ws, n, _handle(stream))
+    _check(st, "spconv_cached_attention")
 
 
 def spconv_forward_plan(m, c_in: int, c_out: int, dtype: int, opt: Options | None = None) -> PlanInfo:
@@ -483,7 +548,9 @@ def _load_ops():
         ops = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(ops)
         ops.bind(*(ctypes.cast(getattr(lib(), f), ctypes.c_void_p).value for f in (
-            "spconv_rms_norm", "spconv_scaled_linear", "spconv_attention", "spconv_attention_workspace_bytes")), _check)
+            "spconv_rms_norm", "spconv_scaled_linear", "spconv_attention", "spconv_attention_workspace_bytes",
+            "spconv_rotate_heads", "spconv_cache_write", "spconv_cache_read", "spconv_cached_attention",
+            "spconv_cached_attention_workspace_bytes")), _check)
         _ops = ops
     return _ops
 
@@ -537,3 +604,99 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_start: torch.
             return attention(q, k, v, q_start, k_start, max_q, max_k, k_len, prefix, causal, scale, cap, slopes, q_pos, k_pos)
     return (_ops or _load_ops()).attention(q, k, v, q_start, k_start, max_q, max_k, k_len, prefix, causal, scale, cap,
                                            slopes, q_pos, k_pos)
+
+
+def rotary_frequencies(width: int, base: float = 10_000.0, factor: float = 1.0, trained: int = 0, fast: float = 32.0,
+                       slow: float = 1.0, device="cuda") -> tuple[torch.Tensor, float]:
+    """(radians a position of each of width / 2 pairs, float64; gain) for rotate_heads: base^(-2 j / width).
+
+    With a factor above 1, for contexts that many times longer than trained on: without ``trained`` all
+    frequencies are divided by it; with ``trained`` places, pairs that turn more than ``fast`` times in
+    them are kept, those under ``slow`` divided, and a line in the number of turns leads from one to the other,
+    with a gain of 0.1 ln(factor) + 1."""
+    if width < 0 or width % 2:
+        raise ValueError(f"width: expected an even number, got {width}")
+    if not (base > 0 and factor >= 1 and trained >= 0 and fast > slow):
+        raise ValueError("expected base > 0, factor >= 1, trained >= 0 and fast > slow")
+    f = float(base) ** (-2.0 * torch.arange(width // 2, dtype=torch.float64) / max(width, 1))
+    if factor == 1:
+        return f.to(device), 1.0
+    if not trained:
+        return (f / factor).to(device), 1.0
+    kept = ((trained * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
+    return (f * (kept + (1.0 - kept) / factor)).to(device), 0.1 * math.log(factor) + 1.0
+
+
+def rotate_heads(q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, freq: torch.Tensor,
+                 q_gamma: torch.Tensor | None = None, k_gamma: torch.Tensor | None = None, eps: float = 1e-6,
+                 interleaved: bool = False, gain: float = 1.0, stream=None):
+    """Norm of each head (where a gamma is given) and rotation by position of queries and keys, as new
+    tensors (q, k) (spconv_rotate_heads in spconv.h).
+
+    q [n][heads][d], k [n][kv_heads][d] or None, slices of a fused product will do; pos int32 [n], or
+    [n][4] voxels (b, x, y, z); freq float64 [rotated / 2], as rotary_frequencies gives it."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rotate_heads(q, k, pos, freq, q_gamma, k_gamma, eps, interleaved, gain)
+    return (_ops or _load_ops()).rotate_heads(q, k, pos, freq, q_gamma, k_gamma, eps, interleaved, gain)
+
+
+@dataclass
+class Pages:
+    """A cache of pages (spconv_pages in spconv.h): k, v [pages][kv_heads][page][d] in the rows' type, or
+    e4m3 with scales float32 [pages][kv_heads][page].  Which document has which pages is a table, int32
+    [docs][most pages], of the caller's."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+    @classmethod
+    def make(cls, pages: int, page: int, kv_heads: int, head_dim: int, dtype: torch.dtype, bits8: bool = False,
+             device="cuda") -> "Pages":
+        """Pages of zeros."""
+        shape = (pages, kv_heads, page, head_dim)
+        if not bits8:
+            return cls(*(torch.zeros(shape, dtype=dtype, device=device) for _ in range(2)))
+        return cls(*(torch.zeros(shape, dtype=torch.uint8, device=device).view(E4M3) for _ in range(2)),
+                   *(torch.full(shape[:3], 2.0 ** -126, device=device) for _ in range(2)))
+
+    @property
+    def page(self) -> int:
+        return self.k.shape[2]
+
+
+def cache_write(cache: Pages, k: torch.Tensor, v: torch.Tensor, q_start: torch.Tensor, k_len: torch.Tensor,
+                table: torch.Tensor, stream=None) -> None:
+    """New tokens' keys and values [n][kv_heads][d] into the pages of their documents (spconv_cache_write in
+    spconv.h): document t has the rows q_start[t] .. q_start[t + 1], and k_len[t] keys with them."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return cache_write(cache, k, v, q_start, k_len, table)
+    return (_ops or _load_ops()).cache_write(cache.k, cache.v, cache.k_scale, cache.v_scale, k, v, q_start, k_len, table)
+
+
+def cache_read(cache: Pages, start: torch.Tensor, table: torch.Tensor, rows: int, dtype: torch.dtype,
+               stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(k, v) [rows][kv_heads][d] in ``dtype``: rows start[t] .. start[t + 1] get document t's first keys and values
+    (spconv_cache_read in spconv.h); rows of no document are not set."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return cache_read(cache, start, table, rows, dtype)
+    return (_ops or _load_ops()).cache_read(cache.k, cache.v, cache.k_scale, cache.v_scale, start, table, rows, dtype)
+
+
+def cached_attention(q: torch.Tensor, cache: Pages, q_start: torch.Tensor, k_len: torch.Tensor, table: torch.Tensor,
+                     max_q: int, max_k: int, prefix: torch.Tensor | None = None, causal: bool = True,
+                     scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
+                     stream=None) -> torch.Tensor:
+    """Attention of new tokens over the pages of their documents (spconv_cached_attention in spconv.h).
+
+    q [n_q][heads][d]; q_start int32 [docs + 1]; k_len int32 [docs], the new tokens included; table int32
+    [docs][most pages]; scale defaults to 1 / sqrt(d).  Returns [n_q][heads][d]; rows of no document and
+    queries behind max_q are not set."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return cached_attention(q, cache, q_start, k_len, table, max_q, max_k, prefix, causal, scale, cap, slopes)
+    return (_ops or _load_ops()).cached_attention(cache.k, cache.v, cache.k_scale, cache.v_scale, q, q_start, k_len, table,
+                                                  max_q, max_k, prefix, causal, scale, cap, slopes)

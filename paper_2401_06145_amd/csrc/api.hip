@@ -12,6 +12,8 @@
 #include <vector>
 
 #include "attention.h"
+#include "pages.h"
+#include "rotate.h"
 #include "common.h"
 #include "spconv.h"
 
@@ -93,7 +95,7 @@ const char* prof_name(int id) {
       "k_minmax", "k_radix_hist", "k_radix_scatter", "k_scan", "k_copy", "k_down_keys", "k_unique", "k_backward",
       "k_forward_count", "k_forward_write", "k_fill", "k_radix_local", "k_gather", "k_gemm", "k_scatter", "k_pack",
       "k_hash_insert", "k_hash_probe", "k_scatter_centre", "k_conv_small", "k_rms_norm", "k_scaled_linear", "k_attention",
-      "k_attention_join"};
+      "k_attention_join", "k_rotate", "k_cache_write", "k_cache_read"};
   return (id >= 0 && id < PROF_IDS) ? kNames[id] : "";
 }
 struct PhaseRec {
@@ -1168,6 +1170,75 @@ size_t attention_bytes(const spconv_attention_args* a, const AttnPlan& p, void* 
   return b.off;
 }
 
+// What both attention calls give their kernels, keys and the split of the launch apart.
+AttnArgs attention_common(const spconv_attention_args* a, const AttnPlan& p) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  AttnArgs k = {};
+  k.q = a->d_q, k.out = a->d_out;
+  k.q_row = a->q_row, k.q_head = a->q_head, k.out_row = a->out_row, k.out_head = a->out_head;
+  k.q_start = a->d_q_start, k.k_len = a->d_k_len, k.prefix = a->d_prefix, k.slopes = a->d_slopes;
+  k.n_q = a->n_q, k.n_docs = a->n_docs, k.max_q = a->max_q, k.max_k = a->max_k;
+  k.heads = a->heads, k.kv_heads = a->kv_heads, k.d = a->head_dim, k.causal = a->causal;
+  if (a->cap > 0.0f) set_cap(&k, a->cap, a->scale, a->dtype == SPCONV_F32);
+  k.slope_by = a->cap > 0.0f ? kLog2e : 1.0f / a->scale;
+  k.exp_by = a->cap > 0.0f ? 1.0f : a->scale * kLog2e;
+  // below every finite score that matters, and finite in both units
+  k.floor = -3e38f / std::max(1.0f, k.exp_by);
+  k.slots = (int)p.slots, k.splits = p.splits, k.chunk = p.chunk;
+  return k;
+}
+
+constexpr int kMostPage = 1 << 16;
+
+// A cache of pages for rows of `dtype`; `n` rows of the call (no pointers are needed for none).
+int check_pages(const spconv_pages* p, int dtype, int64_t n) {
+  if (!p) return fail(SPCONV_EINVAL, "pages is NULL");
+  if (!known_dtype(dtype)) return fail(SPCONV_EUNSUPPORTED, "dtype");
+  if (n < 0 || p->n_pages < 0 || p->n_docs < 0 || p->table_row < 0) return fail(SPCONV_EINVAL, "negative size");
+  if (n > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (p->n_pages > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 pages");
+  if (p->kv_heads <= 0) return fail(SPCONV_EINVAL, "no key heads");
+  if (p->kv_heads > 65535) return fail(SPCONV_EUNSUPPORTED, "more than 65535 heads");
+  if ((p->d_k_scale == nullptr) != (p->d_v_scale == nullptr))
+    return fail(SPCONV_EINVAL, "scales are given for keys and values, or for neither");
+  if (p->head_dim < 8 || p->head_dim > 256 || p->head_dim % (p->d_k_scale ? 16 : 8) != 0)
+    return fail(SPCONV_EUNSUPPORTED, "head_dim must be a multiple of 8 (8-bit pages: of 16) up to 256");
+  if (p->page < 1 || p->page > kMostPage || (p->page & (p->page - 1)) != 0)
+    return fail(SPCONV_EUNSUPPORTED, "rows of a page must be a power of two up to 65536");
+  if ((int64_t)p->table_row * p->page > 1 << 30) return fail(SPCONV_EUNSUPPORTED, "more than 2^30 keys in a document");
+  if (n == 0 || p->n_docs == 0) return SPCONV_OK;
+  if ((p->n_pages > 0 && (!p->d_k || !p->d_v)) || (p->table_row > 0 && !p->d_table)) return fail(SPCONV_EINVAL, "NULL pointer");
+  if (misaligned16(p->d_k) || misaligned16(p->d_v)) return fail(SPCONV_EINVAL, "pages must be 16-byte aligned");
+  for (const void* q : {(const void*)p->d_k_scale, (const void*)p->d_v_scale, (const void*)p->d_table})
+    if (reinterpret_cast<uintptr_t>(q) % 4 != 0) return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
+  return SPCONV_OK;
+}
+
+PageArgs page_args(const spconv_pages* p) {
+  return PageArgs{p->d_k, p->d_v, p->d_k_scale, p->d_v_scale, p->d_table, p->n_docs, p->table_row, (int)p->n_pages,
+                  __builtin_ctz((unsigned)p->page), p->kv_heads, p->head_dim};
+}
+
+// Rows outside of the pages, keys and values.
+int check_rows(const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head, int dtype) {
+  if (!k || !v) return fail(SPCONV_EINVAL, "NULL pointer");
+  if (misaligned16(k) || misaligned16(v)) return fail(SPCONV_EINVAL, "rows must be 16-byte aligned");
+  for (int64_t stride : {k_row, k_head, v_row, v_head})
+    if (stride < 0 || stride * (int64_t)elem_bytes(dtype) % 16 != 0)
+      return fail(SPCONV_EUNSUPPORTED, "strides must be multiples of 16 bytes");
+  return SPCONV_OK;
+}
+
+int check_cached_attention(const spconv_pages* p, const spconv_attention_args* a) {
+  int st = check_attention(a);
+  if (st != SPCONV_OK) return st;
+  if ((st = check_pages(p, a->dtype, 0)) != SPCONV_OK) return st;
+  if (p->kv_heads != a->kv_heads || p->head_dim != a->head_dim || p->n_docs != a->n_docs)
+    return fail(SPCONV_EINVAL, "pages and queries differ in key heads, head_dim or documents");
+  if (a->d_q_pos) return fail(SPCONV_EUNSUPPORTED, "pages hold no voxels");
+  return SPCONV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1242,25 +1313,108 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
   if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
     return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
   const AttnPlan p = plan_of(a);
-  AttnArgs k = {};
+  AttnArgs k = attention_common(a, p);
   const size_t need = attention_bytes(a, p, d_workspace, &k.part_ml, &k.part_o);
   if (need > 0 && (!d_workspace || ws_bytes < need)) return fail(SPCONV_ENOSPC, "attention workspace too small");
   if (reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0) return fail(SPCONV_EINVAL, "workspace must be 256-byte aligned");
-  constexpr float kLog2e = 1.4426950408889634f;
-  k.q = a->d_q, k.k = a->d_k, k.v = a->d_v, k.out = a->d_out;
-  k.q_row = a->q_row, k.q_head = a->q_head, k.k_row = a->k_row, k.k_head = a->k_head;
-  k.v_row = a->v_row, k.v_head = a->v_head, k.out_row = a->out_row, k.out_head = a->out_head;
-  k.q_start = a->d_q_start, k.k_start = a->d_k_start, k.k_len = a->d_k_len, k.prefix = a->d_prefix;
-  k.slopes = a->d_slopes, k.q_pos = a->d_q_pos, k.k_pos = a->d_k_pos;
-  k.n_q = a->n_q, k.n_k = a->n_k, k.n_docs = a->n_docs, k.max_q = a->max_q, k.max_k = a->max_k;
-  k.heads = a->heads, k.kv_heads = a->kv_heads, k.d = a->head_dim, k.causal = a->causal;
-  if (a->cap > 0.0f) set_cap(&k, a->cap, a->scale, a->dtype == SPCONV_F32);
-  k.slope_by = a->cap > 0.0f ? kLog2e : 1.0f / a->scale;
-  k.exp_by = a->cap > 0.0f ? 1.0f : a->scale * kLog2e;
-  // below every finite score that matters, and finite in both units
-  k.floor = -3e38f / std::max(1.0f, k.exp_by);
-  k.slots = (int)p.slots, k.splits = p.splits, k.chunk = p.chunk;
+  k.k = a->d_k, k.v = a->d_v;
+  k.k_row = a->k_row, k.k_head = a->k_head, k.v_row = a->v_row, k.v_head = a->v_head;
+  k.k_start = a->d_k_start, k.q_pos = a->d_q_pos, k.k_pos = a->d_k_pos, k.n_k = a->n_k;
   return launched(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention");
+}
+
+size_t spconv_cached_attention_workspace_bytes(const spconv_pages* pages, const spconv_attention_args* a) {
+  if (check_cached_attention(pages, a) != SPCONV_OK) return 0;
+  return attention_bytes(a, plan_of(a), nullptr, nullptr, nullptr);
+}
+
+int spconv_cached_attention(const spconv_pages* pages, const spconv_attention_args* a, void* d_workspace, size_t ws_bytes,
+                            void* stream) {
+  int st = check_cached_attention(pages, a);
+  if (st != SPCONV_OK) return st;
+  if (a->n_q == 0 || a->n_docs == 0) return SPCONV_OK;
+  if ((st = check_pages(pages, a->dtype, a->n_q)) != SPCONV_OK) return st;
+  if (a->max_q == 0) return fail(SPCONV_EINVAL, "max_q is 0 but there are queries");
+  if (!a->d_q || !a->d_out || !a->d_q_start || !a->d_k_len) return fail(SPCONV_EINVAL, "NULL pointer");
+  if (misaligned16(a->d_q) || misaligned16(a->d_out)) return fail(SPCONV_EINVAL, "d_q and d_out must be 16-byte aligned");
+  const int64_t e = elem_bytes(a->dtype);
+  for (int64_t stride : {a->q_row, a->q_head, a->out_row, a->out_head})
+    if (stride < 0 || stride * e % 16 != 0) return fail(SPCONV_EUNSUPPORTED, "strides must be multiples of 16 bytes");
+  if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
+    return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
+  const AttnPlan p = plan_of(a);
+  AttnArgs k = attention_common(a, p);
+  const size_t need = attention_bytes(a, p, d_workspace, &k.part_ml, &k.part_o);
+  if (need > 0 && (!d_workspace || ws_bytes < need)) return fail(SPCONV_ENOSPC, "attention workspace too small");
+  if (reinterpret_cast<uintptr_t>(d_workspace) % 256 != 0) return fail(SPCONV_EINVAL, "workspace must be 256-byte aligned");
+  const PageArgs pg = page_args(pages);
+  k.k = pg.k, k.v = pg.v, k.k_scale = pg.k_scale, k.v_scale = pg.v_scale;
+  k.paged = 1, k.table = pg.table, k.table_row = pg.table_row, k.n_pages = pg.n_pages, k.shift = pg.shift;
+  k.n_k = (int64_t)pg.table_row << pg.shift;
+  return launched(launch_attention(k, p, a->dtype, static_cast<hipStream_t>(stream)), "attention over pages");
+}
+
+int spconv_cache_write(const spconv_pages* pages, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
+                       int64_t v_row, int64_t v_head, const int32_t* d_q_start, const int32_t* d_k_len, int64_t n,
+                       int dtype, void* stream) {
+  int st = check_pages(pages, dtype, n);
+  if (st != SPCONV_OK || n == 0 || pages->n_docs == 0) return st;
+  if ((st = check_rows(d_k, k_row, k_head, d_v, v_row, v_head, dtype)) != SPCONV_OK) return st;
+  if (!d_q_start || !d_k_len) return fail(SPCONV_EINVAL, "NULL pointer");
+  return launched(launch_cache(page_args(pages), HeadRows{const_cast<void*>(d_k), k_row, k_head},
+                               HeadRows{const_cast<void*>(d_v), v_row, v_head}, d_q_start, d_k_len, n, dtype,
+                               static_cast<hipStream_t>(stream)),
+                  "cache write");
+}
+
+int spconv_cache_read(const spconv_pages* pages, void* d_k, int64_t k_row, int64_t k_head, void* d_v, int64_t v_row,
+                      int64_t v_head, const int32_t* d_start, int64_t n, int dtype, void* stream) {
+  int st = check_pages(pages, dtype, n);
+  if (st != SPCONV_OK || n == 0 || pages->n_docs == 0) return st;
+  if ((st = check_rows(d_k, k_row, k_head, d_v, v_row, v_head, dtype)) != SPCONV_OK) return st;
+  for (int64_t row : {k_row, v_row})
+    if (n > 1 && row < pages->head_dim) return fail(SPCONV_EINVAL, "rows of the output overlap");
+  for (int64_t head : {k_head, v_head})
+    if (pages->kv_heads > 1 && head < pages->head_dim) return fail(SPCONV_EINVAL, "heads of the output overlap");
+  if (!d_start) return fail(SPCONV_EINVAL, "NULL pointer");
+  return launched(launch_cache(page_args(pages), HeadRows{d_k, k_row, k_head}, HeadRows{d_v, v_row, v_head}, d_start, nullptr,
+                               n, dtype, static_cast<hipStream_t>(stream)),
+                  "cache read");
+}
+
+int spconv_rotate_heads(const spconv_rotation* r, void* stream) {
+  if (!r) return fail(SPCONV_EINVAL, "args is NULL");
+  if (!known_dtype(r->dtype)) return fail(SPCONV_EUNSUPPORTED, "dtype");
+  if (r->n < 0 || r->heads <= 0 || r->kv_heads < 0) return fail(SPCONV_EINVAL, "negative size, or no heads");
+  if (r->n > 0x7fffffff) return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  if (r->heads > 65535 || r->kv_heads > 65535) return fail(SPCONV_EUNSUPPORTED, "more than 65535 heads");
+  if (r->head_dim < 1 || r->head_dim > kMostRotated) return fail(SPCONV_EUNSUPPORTED, "head_dim must be 1 to 256");
+  if (r->rotated < 0 || r->rotated > r->head_dim || r->rotated % 2 != 0)
+    return fail(SPCONV_EINVAL, "rotated columns must be an even number, at most head_dim");
+  if (!(r->eps >= 0.0f) || !std::isfinite(r->eps)) return fail(SPCONV_EINVAL, "eps must be finite and not negative");
+  if (!std::isfinite(r->gain)) return fail(SPCONV_EINVAL, "gain must be finite");
+  if (r->n == 0) return SPCONV_OK;
+  RotateArgs k = {{r->d_q, r->d_k}, {r->d_q_out, r->d_k_out}, {r->q_row, r->k_row}, {r->q_head, r->k_head},
+                  {r->q_out_row, r->k_out_row}, {r->q_out_head, r->k_out_head}, {r->d_q_gamma, r->d_k_gamma}, r->d_pos,
+                  r->d_freq, r->n, {r->heads, r->kv_heads}, r->head_dim, r->rotated, r->voxels != 0, r->eps, r->gain, 1, 1};
+  const uintptr_t e = elem_bytes(r->dtype);
+  for (int i = 0; i < 2; ++i) {
+    if (k.heads[i] == 0) {
+      k.x[i] = nullptr, k.y[i] = nullptr, k.gamma[i] = nullptr;
+      k.x_row[i] = k.x_head[i] = k.y_row[i] = k.y_head[i] = 0;
+      continue;
+    }
+    if (!k.x[i] || !k.y[i]) return fail(SPCONV_EINVAL, "NULL pointer");
+    if (k.x_row[i] < 0 || k.x_head[i] < 0) return fail(SPCONV_EINVAL, "negative stride");
+    if ((r->n > 1 && k.y_row[i] < r->head_dim) || (k.heads[i] > 1 && k.y_head[i] < r->head_dim) || k.y_row[i] < 0 || k.y_head[i] < 0)
+      return fail(SPCONV_EINVAL, "rows or heads of the output overlap");
+    for (const void* p : {k.x[i], (const void*)k.y[i], k.gamma[i]})
+      if (reinterpret_cast<uintptr_t>(p) % e != 0) return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
+  }
+  if (r->rotated > 0 && (!r->d_pos || !r->d_freq)) return fail(SPCONV_EINVAL, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(r->d_pos) % 4 != 0 || reinterpret_cast<uintptr_t>(r->d_freq) % 8 != 0)
+    return fail(SPCONV_EINVAL, "pointer not aligned to its elements");
+  return launched(launch_rotate(k, r->dtype, r->interleaved != 0, static_cast<hipStream_t>(stream)), "rotation");
 }
 
 // --------------------------------------------------------------- measurement

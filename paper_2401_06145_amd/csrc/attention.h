@@ -38,6 +38,11 @@ struct AttnArgs {
   int splits, chunk;  // key ranges, and keys of each
   f32x2* part_ml;     // [splits][n_q][heads] maximum and sum of a range
   float* part_o;      // [splits][n_q][heads][d] its unnormalised output
+  // Keys in pages (pages.h): k and v are theirs, k_row to v_head and k_start not used.
+  const int32_t* table;  // [n_docs][table_row]
+  const float* k_scale;  // NULL: pages hold the rows' type
+  const float* v_scale;
+  int paged, table_row, n_pages, shift;  // paged 0: packed keys
 };
 
 // How a call runs: few queries per document (rows: their columns) or many (slots of query
@@ -51,8 +56,11 @@ struct AttnPlan {
 AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads, int d, int dtype,
                         bool causal);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
-// attention_tile.hip, attention_rows.hip: the two forms.
+// attention_tile.hip, attention_rows.hip: the two forms over packed keys; attention_pages.hip,
+// attention_pages8.hip: both over pages of the rows' type and of 8 bits.
 hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attention_rows(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attention_pages(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attention_pages8(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 
 }  // namespace spc

@@ -204,7 +204,10 @@ hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hip
   if (a.splits > 1 && !fits_launch(a.n_q * a.heads, kWave)) return hipErrorInvalidConfiguration;
   {
     ProfScope ps(KN_ATTENTION, s);
-    const hipError_t e = p.rows ? launch_attention_rows(a, p, dtype, s) : launch_attention_tile(a, p, dtype, s);
+    const hipError_t e = a.k_scale ? launch_attention_pages8(a, p, dtype, s)
+                         : a.paged ? launch_attention_pages(a, p, dtype, s)
+                         : p.rows  ? launch_attention_rows(a, p, dtype, s)
+                                   : launch_attention_tile(a, p, dtype, s);
     if (e != hipSuccess) return e;
   }
   if (a.splits <= 1) return hipSuccess;

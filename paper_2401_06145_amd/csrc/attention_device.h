@@ -140,8 +140,13 @@ __device__ __forceinline__ i16x4 read_columns(const char* p) {
 // product with V, those below 2^-25 of the largest would vanish from the sum of values, but
 // not from the sum of exponentials (131,072 keys at 2^-25.5 beside a dominant one hold 0.3 % of a
 // row).  The factor is part of both sums and leaves with their quotient.
-template <typename T>
-constexpr float kExpRaise = std::is_same_v<T, _Float16> ? 15.0f : 0.0f;
+// 8-bit pages: half of it, as a scale's mantissa (below 2) is multiplied in before the rounding.
+template <typename T, int SRC = 0>
+constexpr float kExpRaise = !std::is_same_v<T, _Float16> ? 0.0f : SRC == 2 ? 14.0f : 15.0f;
+
+// Where keys and values are: rows that follow each other; pages of the rows' type, by a table; pages
+// of 8 bits with a scale for each row.
+enum Source { kPacked = 0, kPages = 1, kPages8 = 2 };
 
 // A document's part of the batch.
 struct Doc {
@@ -149,15 +154,66 @@ struct Doc {
   int64_t k0;
   int len_k, prefix;
 };
+template <int SRC = kPacked>
 __device__ __forceinline__ Doc load_doc(const AttnArgs& a, int doc) {
   Doc d;
   d.q0 = std::max(a.q_start[doc], 0);
   d.len_q = std::min((int)std::min<int64_t>(a.q_start[doc + 1], a.n_q) - d.q0, a.max_q);
-  d.k0 = std::max(a.k_start[doc], 0);
-  const int64_t len = a.k_len ? a.k_len[doc] : a.k_start[doc + 1] - d.k0;
+  int64_t len;
+  if constexpr (SRC == kPacked) {
+    d.k0 = std::max(a.k_start[doc], 0);
+    len = a.k_len ? a.k_len[doc] : a.k_start[doc + 1] - d.k0;
+  } else {
+    d.k0 = 0;
+    len = a.k_len[doc];
+  }
   d.len_k = (int)std::max<int64_t>(0, std::min<int64_t>(std::min<int64_t>(len, a.max_k), a.n_k - d.k0));
   d.prefix = a.prefix ? a.prefix[doc] : 0;
   return d;
+}
+
+// 8-bit rows.  Keys' scales multiply the scores.  A value's scale is split: its power of two goes with
+// the conversion to 16 bits, which it leaves exact (four significant bits; float16 subnormals apart,
+// which such rows would lose in float16 pages too), and the rest, from 1 to below 2, into the
+// exponential before that is rounded.  One that is not finite stands for rows of NaN.
+struct Scale {
+  float power, rest;
+};
+template <typename T>
+__device__ __forceinline__ Scale split_scale(float s) {
+  const bool finite = s < INFINITY;
+  if constexpr (sizeof(T) == 4) return Scale{1.0f, finite ? s : NAN};
+  const uint32_t bits = __builtin_bit_cast(uint32_t, s);
+  return Scale{finite ? __builtin_bit_cast(float, bits & 0x7f800000u) : 1.0f,
+               finite ? __builtin_bit_cast(float, (bits & 0x007fffffu) | 0x3f800000u) : NAN};
+}
+// Eight e4m3 numbers times a power of two (16-bit types) as a fragment.
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag from_e4m3(uint32_t lo, uint32_t hi, float power) {
+  if constexpr (sizeof(T) == 4) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
+    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+    return f32x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  } else if constexpr (std::is_same_v<T, _Float16>) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, power, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, power, true);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  } else {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+
+// The page that holds a document's key `place`, or -1: none, whose rows count as zeros.
+__device__ __forceinline__ int page_at(const AttnArgs& a, int doc, const Doc& d, int place) {
+  if (place >= d.len_k) return -1;
+  const int page = a.table[(int64_t)doc * a.table_row + (place >> a.shift)];
+  return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+}
+// The row of a head's part of that page, among all rows of the pages.
+__device__ __forceinline__ int64_t row_of(const AttnArgs& a, int page, int kvh, int place) {
+  return (((int64_t)page * a.kv_heads + kvh) << a.shift) + (place & ((1 << a.shift) - 1));
 }
 // Number of keys that query i sees: the first ones of its document.
 __device__ __forceinline__ int seen(const AttnArgs& a, const Doc& d, int i) {

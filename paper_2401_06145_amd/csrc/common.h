@@ -107,8 +107,8 @@ enum ProfId : int {
   KN_MINMAX = 16, KN_RADIX_HIST, KN_RADIX_SCATTER, KN_SCAN, KN_COPY, KN_DOWN_KEYS, KN_UNIQUE,
   KN_BACKWARD, KN_FORWARD_COUNT, KN_FORWARD_WRITE, KN_FILL, KN_RADIX_LOCAL, KN_GATHER, KN_GEMM, KN_SCATTER,
   KN_PACK, KN_HASH_INSERT, KN_HASH_PROBE, KN_SCATTER_CENTRE, KN_CONV_SMALL,
-  KN_RMS_NORM, KN_SCALED_LINEAR, KN_ATTENTION, KN_ATTENTION_JOIN,
-  PROF_IDS = 40
+  KN_RMS_NORM, KN_SCALED_LINEAR, KN_ATTENTION, KN_ATTENTION_JOIN, KN_ROTATE, KN_CACHE_WRITE, KN_CACHE_READ,
+  PROF_IDS = 43
 };
 struct ProfScope {
   void* rec = nullptr;
@@ -318,6 +318,6 @@ constexpr int64_t kMostLinearStride = 1 << 23;
 hipError_t launch_scaled_linear(const void* x, int64_t ld_x, const float* xs, int64_t ld_xs, const void* w, int64_t ld_w,
                                 const float* ws, int64_t ld_ws, void* y, int64_t ld_y, int64_t m, int n, int k, int dtype,
                                 int relu, bool exact, hipStream_t s);
-// (attention.hip: attention.h)
+// (attention.hip: attention.h; rotate.hip: rotate.h; cache.hip: pages.h)
 
 }  // namespace spc

@@ -27,26 +27,38 @@ struct Api {
   decltype(&spconv_scaled_linear) scaled_linear = nullptr;
   decltype(&spconv_attention) attention = nullptr;
   decltype(&spconv_attention_workspace_bytes) workspace = nullptr;
+  decltype(&spconv_rotate_heads) rotate_heads = nullptr;
+  decltype(&spconv_cache_write) cache_write = nullptr;
+  decltype(&spconv_cache_read) cache_read = nullptr;
+  decltype(&spconv_cached_attention) cached_attention = nullptr;
+  decltype(&spconv_cached_attention_workspace_bytes) cached_workspace = nullptr;
   PyObject* check = nullptr;  // (status, name): raises the library's error
 } api;
 
-// bind(rms_norm, scaled_linear, attention, attention_workspace_bytes, check): the library's
-// functions, as addresses.
+// bind(functions..., check): the library's functions as addresses, in the order of Api.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 5 arguments");
+  constexpr int kFunctions = 9;
+  if (n != kFunctions + 1) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 10 arguments");
     return nullptr;
   }
-  void* at[4];
-  for (int i = 0; i < 4; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+  void* at[kFunctions];
+  for (int i = 0; i < kFunctions; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
   if (PyErr_Occurred()) return nullptr;
-  api.rms_norm = reinterpret_cast<decltype(api.rms_norm)>(at[0]);
-  api.scaled_linear = reinterpret_cast<decltype(api.scaled_linear)>(at[1]);
-  api.attention = reinterpret_cast<decltype(api.attention)>(at[2]);
-  api.workspace = reinterpret_cast<decltype(api.workspace)>(at[3]);
+  int i = 0;
+  const auto take = [&](auto& f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(at[i++]); };
+  take(api.rms_norm);
+  take(api.scaled_linear);
+  take(api.attention);
+  take(api.workspace);
+  take(api.rotate_heads);
+  take(api.cache_write);
+  take(api.cache_read);
+  take(api.cached_attention);
+  take(api.cached_workspace);
   Py_XDECREF(api.check);
-  Py_INCREF(args[4]);
-  api.check = args[4];
+  Py_INCREF(args[kFunctions]);
+  api.check = args[kFunctions];
   Py_RETURN_NONE;
 }
 
@@ -271,12 +283,198 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count) {
   SPC_END
 }
 
-PyMethodDef methods[] = {
-    {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
-    {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm)), METH_FASTCALL, nullptr},
-    {"scaled_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(scaled_linear)), METH_FASTCALL, nullptr},
-    {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention)), METH_FASTCALL, nullptr},
-    {nullptr, nullptr, 0, nullptr}};
+// rotate_heads(q, k or None, pos, freq, q_gamma, k_gamma, eps, interleaved, gain) -> (q, k or None)
+PyObject* rotate_heads(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  SPC_BEGIN
+  if (count != 9) throw Refused("rotate_heads takes 9 arguments");
+  const at::Tensor &q = get(args[0], "q"), &pos = get(args[2], "pos"), &freq = get(args[3], "freq");
+  if (q.dim() != 3) refuse("q", "[rows][heads][width]", q);
+  const at::ScalarType t = q.scalar_type();
+  spconv_rotation r = {};
+  r.dtype = dtype_of(t, "q");
+  const int64_t n = q.size(0), d = q.size(2);
+  heads(q, "q", t, d);
+  const at::Tensor* k = args[1] == Py_None ? nullptr : &get(args[1], "k");
+  if (k) {
+    heads(*k, "k", t, d);
+    if (k->size(0) != n) refuse("k", "as many rows as q", *k);
+  }
+  if (pos.dim() < 1 || pos.dim() > 2) refuse("pos", "contiguous Int [rows] or [rows][4]", pos);
+  if (freq.dim() != 1) refuse("freq", "contiguous Double [rotated / 2]", freq);
+  if (q.size(1) > INT32_MAX || d > INT32_MAX || freq.size(0) > INT32_MAX / 2 || (k && k->size(1) > INT32_MAX))
+    throw Refused("sizes of more than 31 bits");
+  r.n = n, r.heads = (int)q.size(1), r.kv_heads = k ? (int)k->size(1) : 0, r.head_dim = (int)d;
+  r.rotated = 2 * (int)freq.size(0);
+  r.voxels = pos.dim() == 2;
+  r.d_pos = r.voxels ? array<int32_t>(args[2], "pos", at::kInt, {n, 4}, q.device())
+                     : array<int32_t>(args[2], "pos", at::kInt, {n}, q.device());
+  r.d_freq = array<double>(args[3], "freq", at::kDouble, {freq.size(0)}, q.device());
+  r.d_q_gamma = array<void>(args[4], "q_gamma", t, {d}, q.device());
+  r.d_k_gamma = array<void>(args[5], "k_gamma", t, {d}, q.device());
+  r.eps = real(args[6]), r.interleaved = truth(args[7]), r.gain = real(args[8]);
+  same_device(q, {k});
+  const c10::OptionalDeviceGuard guard(q.device());
+  at::Tensor q_out = empty(q.sizes(), t, q), k_out;
+  if (k) k_out = empty(k->sizes(), t, q);
+  const auto place = [](const at::Tensor& x, int64_t* row, int64_t* head) {
+    const Strides s = strides(x);
+    *row = s.row, *head = s.head;
+  };
+  r.d_q = q.data_ptr(), r.d_q_out = q_out.data_ptr();
+  place(q, &r.q_row, &r.q_head);
+  place(q_out, &r.q_out_row, &r.q_out_head);
+  if (k) {
+    r.d_k = k->data_ptr(), r.d_k_out = k_out.data_ptr();
+    place(*k, &r.k_row, &r.k_head);
+    place(k_out, &r.k_out_row, &r.k_out_head);
+  }
+  if (failed(api.rotate_heads(&r, stream_of(q)), "spconv_rotate_heads")) return nullptr;
+  PyObject* out = PyTuple_New(2);
+  if (!out) return nullptr;
+  PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(q_out)));
+  PyTuple_SET_ITEM(out, 1, k ? THPVariable_Wrap(std::move(k_out)) : (Py_INCREF(Py_None), Py_None));
+  return out;
+  SPC_END
+}
+
+// The pages of args[0..3] (keys, values, their scales or None), and the table args[table].
+struct Pages {
+  spconv_pages p = {};
+  const at::Tensor* k;
+  bool bits8;
+};
+Pages get_pages(PyObject* const* args, PyObject* table_arg) {
+  Pages g;
+  const at::Tensor &k = get(args[0], "pages of keys"), &v = get(args[1], "pages of values"), &table = get(table_arg, "table");
+  g.k = &k;
+  if (k.dim() != 4) refuse("pages of keys", "[pages][heads][rows][width]", k);
+  g.bits8 = k.scalar_type() == at::kFloat8_e4m3fn;
+  const int64_t pages = k.size(0), heads = k.size(1), page = k.size(2), d = k.size(3);
+  if (heads > INT32_MAX || page > INT32_MAX || d > INT32_MAX) throw Refused("sizes of more than 31 bits");
+  if (v.scalar_type() != k.scalar_type() || v.sizes() != k.sizes()) refuse("pages of values", "the keys' shape and type", v);
+  if (!k.is_contiguous() || !v.is_contiguous()) throw Refused("pages: not contiguous");
+  if ((args[2] != Py_None) != g.bits8 || (args[3] != Py_None) != g.bits8)
+    throw Refused("scales belong to pages of 8 bits (Float8_e4m3fn), and to no others");
+  if (v.device() != k.device()) throw Refused("tensors on different devices");
+  g.p.d_k = k.data_ptr(), g.p.d_v = v.data_ptr();
+  g.p.d_k_scale = const_cast<float*>(array<float>(args[2], "scales of keys", at::kFloat, {pages, heads, page}, k.device()));
+  g.p.d_v_scale = const_cast<float*>(array<float>(args[3], "scales of values", at::kFloat, {pages, heads, page}, k.device()));
+  if (table.dim() != 2 || table.size(0) > INT32_MAX || table.size(1) > INT32_MAX) refuse("table", "contiguous Int [docs][pages]", table);
+  g.p.d_table = array<int32_t>(table_arg, "table", at::kInt, {table.size(0), table.size(1)}, k.device());
+  g.p.n_pages = pages, g.p.n_docs = (int)table.size(0), g.p.table_row = (int)table.size(1);
+  g.p.page = (int)page, g.p.kv_heads = (int)heads, g.p.head_dim = (int)d;
+  // no page has no address, but is still one of 8 bits
+  static float nothing;
+  if (g.bits8 && !g.p.d_k_scale) g.p.d_k_scale = g.p.d_v_scale = &nothing;
+  return g;
+}
+void same_type(const Pages& g, at::ScalarType t) {
+  if (!g.bits8 && g.k->scalar_type() != t)
+    throw Refused(std::string("pages of ") + c10::toString(g.k->scalar_type()) + " and rows of " + c10::toString(t));
+}
+
+// cache_write(pages of keys, of values, scales of keys, of values, k, v, q_start, k_len, table)
+PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  SPC_BEGIN
+  if (count != 9) throw Refused("cache_write takes 9 arguments");
+  const Pages g = get_pages(args, args[8]);
+  const at::Tensor &k = get(args[4], "k"), &v = get(args[5], "v");
+  const at::ScalarType t = k.scalar_type();
+  const int dtype = dtype_of(t, "k");
+  same_type(g, t);
+  heads(k, "k", t, g.p.head_dim);
+  heads(v, "v", t, g.p.head_dim);
+  if (k.size(1) != g.p.kv_heads) refuse("k", "the pages' heads", k);
+  if (v.sizes() != k.sizes()) refuse("v", "k's shape", v);
+  const int64_t docs = g.p.n_docs;
+  get(args[6], "q_start"), get(args[7], "k_len");
+  const int32_t* start = array<int32_t>(args[6], "q_start", at::kInt, {docs + 1}, k.device());
+  const int32_t* len = array<int32_t>(args[7], "k_len", at::kInt, {docs}, k.device());
+  same_device(k, {&v, g.k});
+  const c10::OptionalDeviceGuard guard(k.device());
+  const Strides sk = strides(k), sv = strides(v);
+  if (failed(api.cache_write(&g.p, k.data_ptr(), sk.row, sk.head, v.data_ptr(), sv.row, sv.head, start, len, k.size(0), dtype,
+                             stream_of(k)),
+             "spconv_cache_write"))
+    return nullptr;
+  Py_RETURN_NONE;
+  SPC_END
+}
+
+// cache_read(pages of keys, of values, scales of keys, of values, start, table, rows, dtype) -> (k, v)
+PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  SPC_BEGIN
+  if (count != 8) throw Refused("cache_read takes 8 arguments");
+  const Pages g = get_pages(args, args[5]);
+  if (!THPDtype_Check(args[7])) throw Refused("dtype: expected a torch.dtype");
+  const at::ScalarType t = reinterpret_cast<THPDtype*>(args[7])->scalar_type;
+  const int dtype = dtype_of(t, "dtype");
+  same_type(g, t);
+  get(args[4], "start");
+  const int32_t* start = array<int32_t>(args[4], "start", at::kInt, {(int64_t)g.p.n_docs + 1}, g.k->device());
+  const int64_t rows = whole(args[6]);
+  if (rows < 0) throw Refused("rows: negative");
+  same_device(*g.k, {});
+  const c10::OptionalDeviceGuard guard(g.k->device());
+  at::Tensor k = empty({rows, g.p.kv_heads, g.p.head_dim}, t, *g.k), v = empty(k.sizes(), t, *g.k);
+  const Strides s = strides(k);
+  if (failed(api.cache_read(&g.p, k.data_ptr(), s.row, s.head, v.data_ptr(), s.row, s.head, start, rows, dtype, stream_of(*g.k)),
+             "spconv_cache_read"))
+    return nullptr;
+  PyObject* out = PyTuple_New(2);
+  if (!out) return nullptr;
+  PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(std::move(k)));
+  PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(std::move(v)));
+  return out;
+  SPC_END
+}
+
+// cached_attention(pages of keys, of values, scales of keys, of values, q, q_start, k_len, table, max_q, max_k,
+//                  prefix, causal, scale or None, cap, slopes) -> out
+PyObject* cached_attention(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  SPC_BEGIN
+  if (count != 15) throw Refused("cached_attention takes 15 arguments");
+  const Pages g = get_pages(args, args[7]);
+  const at::Tensor& q = get(args[4], "q");
+  if (q.dim() != 3) refuse("q", "[rows][heads][width]", q);
+  const at::ScalarType t = q.scalar_type();
+  spconv_attention_args a = {};
+  a.dtype = dtype_of(t, "q");
+  same_type(g, t);
+  heads(q, "q", t, g.p.head_dim);
+  const int64_t docs = g.p.n_docs;
+  if (q.size(1) > INT32_MAX) throw Refused("sizes of more than 31 bits");
+  a.n_q = q.size(0), a.n_docs = g.p.n_docs;
+  a.heads = (int)q.size(1), a.kv_heads = g.p.kv_heads, a.head_dim = g.p.head_dim;
+  get(args[5], "q_start"), get(args[6], "k_len");
+  a.d_q_start = array<int32_t>(args[5], "q_start", at::kInt, {docs + 1}, q.device());
+  a.d_k_len = array<int32_t>(args[6], "k_len", at::kInt, {docs}, q.device());
+  a.max_q = whole(args[8]), a.max_k = whole(args[9]);
+  a.d_prefix = array<int32_t>(args[10], "prefix", at::kInt, {docs}, q.device());
+  a.causal = truth(args[11]);
+  a.scale = args[12] == Py_None ? (float)(1.0 / std::sqrt((double)a.head_dim)) : real(args[12]);
+  a.cap = real(args[13]);
+  a.d_slopes = array<float>(args[14], "slopes", at::kFloat, {q.size(1)}, q.device());
+  same_device(q, {g.k});
+  const c10::OptionalDeviceGuard guard(q.device());
+  at::Tensor out = empty(q.sizes(), t, q);
+  a.d_q = q.data_ptr(), a.d_out = out.data_ptr();
+  const Strides sq = strides(q), so = strides(out);
+  a.q_row = sq.row, a.q_head = sq.head, a.out_row = so.row, a.out_head = so.head;
+  const size_t need = api.cached_workspace(&g.p, &a);
+  at::Tensor workspace;
+  if (need) workspace = empty({(int64_t)need}, at::kByte, q);
+  if (failed(api.cached_attention(&g.p, &a, need ? workspace.data_ptr() : nullptr, need, stream_of(q)),
+             "spconv_cached_attention"))
+    return nullptr;
+  return THPVariable_Wrap(std::move(out));
+  SPC_END
+}
+
+#define SPC_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {SPC_METHOD(bind), SPC_METHOD(rms_norm), SPC_METHOD(scaled_linear), SPC_METHOD(attention),
+                         SPC_METHOD(rotate_heads), SPC_METHOD(cache_write), SPC_METHOD(cache_read),
+                         SPC_METHOD(cached_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

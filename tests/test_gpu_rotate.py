@@ -1,0 +1,133 @@
+"""spconv_rotate_heads: norm and rotation of heads against 64 bits."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+from paper_2401_06145_amd import binding as B
+from tests import cache_ref as ref
+from tests.gpu_helpers import DEV, say
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+TYPES = [F32, F16, BF16]
+
+
+def inputs(n, hq, hkv, d, dtype, seed=0, fused=True):
+    g = torch.Generator(DEV).manual_seed(seed)
+    rows = torch.randn((n, (hq + 2 * hkv) * d), device=DEV, generator=g).to(dtype)
+    q, k, _ = (t.unflatten(1, (-1, d)) for t in rows.split([hq * d, hkv * d, hkv * d], 1))
+    if not fused:
+        q, k = q.contiguous(), k.contiguous()
+    gammas = [(1 + 0.2 * torch.randn(d, device=DEV, generator=g)).to(dtype) for _ in range(2)]
+    return q, k, gammas
+
+
+def frequencies(rot, base=10_000.0):
+    return B.rotary_frequencies(rot, base, device=DEV)[0]
+
+
+def check(q, k, gammas, pos, freq, what, **kw):
+    gq, gk = gammas
+    got = B.rotate_heads(q, k, pos, freq, q_gamma=gq, k_gamma=gk, **kw)
+    for x, y, gamma, name in ((q, got[0], gq, "q"), (k, got[1], gk, "k")):
+        want, mag = ref.rotate(x, pos, freq, gamma, **kw)
+        assert y.shape == x.shape and y.dtype == x.dtype
+        ref.check_rotated(y, want, mag, f"{what} {name}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(128, 128), (64, 64), (64, 32), (32, 24), (80, 40), (96, 96), (256, 256), (256, 2), (33, 32),
+                                   (20, 20), (16, 6), (8, 8), (2, 2), (1, 0), (255, 254), (192, 64), (128, 0)])
+def test_widths(d, rot, interleaved, dtype):
+    say(f"rotation of {rot} of {d} columns, interleaved {interleaved}, {dtype}")
+    for n, hq, hkv in ((1, 8, 2), (37, 3, 1), (1500, 6, 3)):
+        q, k, gammas = inputs(n, hq, hkv, d, dtype, seed=d + n)
+        pos = torch.arange(n, device=DEV, dtype=torch.int32) * 3 - 40
+        for gs in (gammas, (None, None), (gammas[0], None)):
+            check(q, k, gs, pos, frequencies(rot), f"{n} rows", interleaved=interleaved, gain=1.25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_voxels_and_far_places(dtype):
+    say(f"rotation by voxels and far places {dtype}")
+    g = torch.Generator(DEV).manual_seed(3)
+    q, k, gammas = inputs(700, 8, 2, 32, dtype, seed=3)
+    voxels = 8 * torch.randint(-4000, 4000, (700, 4), device=DEV, generator=g, dtype=torch.int32)
+    for interleaved in (False, True):
+        check(q, k, gammas, voxels, frequencies(24), "voxels", interleaved=interleaved)
+    q, k, gammas = inputs(300, 4, 1, 128, dtype, seed=4)
+    for top in (1 << 20, 1 << 24):
+        far = torch.randint(-top, top, (300,), device=DEV, generator=g, dtype=torch.int32)
+        check(q, k, gammas, far, frequencies(128), f"places up to {top}")
+
+
+def test_frequencies():
+    f, gain = B.rotary_frequencies(8, 10_000.0, device=DEV)
+    assert gain == 1.0 and f.dtype == torch.float64
+    assert torch.allclose(f.cpu(), torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-12)
+    assert torch.equal(B.rotary_frequencies(8, factor=4.0, device=DEV)[0], f / 4)
+    scaled, gain = B.rotary_frequencies(8, factor=4.0, trained=4096, device=DEV)
+    turns = 4096 * f / (2 * math.pi)
+    assert gain == 0.1 * math.log(4.0) + 1.0
+    assert scaled[0] == f[0] and float(turns[0]) > 32      # fast: kept
+    assert scaled[3] == f[3] / 4 and float(turns[3]) < 1   # slow: divided
+    assert f[2] / 4 < scaled[2] < f[2]
+    for bad in (dict(width=7), dict(width=8, factor=0.5), dict(width=8, base=0.0), dict(width=8, slow=40.0)):
+        with pytest.raises(ValueError):
+            B.rotary_frequencies(**bad, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_alignments(dtype):
+    """Rows and heads apart, transposed heads, addresses that no wide access fits; queries alone."""
+    say(f"rotation of strided heads {dtype}")
+    g = torch.Generator(DEV).manual_seed(5)
+    pos, freq = torch.arange(50, device=DEV, dtype=torch.int32), frequencies(64)
+    wide = torch.randn((50, 6, 80), device=DEV, generator=g).to(dtype)
+    turned = torch.randn((4, 50, 64), device=DEV, generator=g).to(dtype).transpose(0, 1)
+    for first in (0, 4, 1, 8):
+        q, k = wide[:, 1:, first:first + 64], turned[:, :2]
+        check(q, k, (None, None), pos, freq, f"columns from {first}")
+        got, none = B.rotate_heads(q, None, pos, freq)
+        assert none is None
+        ref.check_rotated(got, *ref.rotate(q, pos, freq), "queries alone")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_in_place(interleaved):
+    """The C call over its own inputs."""
+    say("rotation in place")
+    q, k, gammas = inputs(300, 8, 2, 64, BF16, seed=6)
+    pos, freq = ref.ints(list(range(300))), frequencies(48)
+    want = B.rotate_heads(q, k, pos, freq, *gammas, interleaved=interleaved)
+    a = B.Rotation(d_q=q.data_ptr(), d_q_out=q.data_ptr(), d_k=k.data_ptr(), d_k_out=k.data_ptr(), n=300, heads=8, kv_heads=2,
+                   head_dim=64, rotated=48, dtype=B.SPCONV_BF16, interleaved=interleaved, eps=1e-6, gain=1.0,
+                   d_pos=pos.data_ptr(), d_freq=freq.data_ptr(), d_q_gamma=gammas[0].data_ptr(), d_k_gamma=gammas[1].data_ptr(),
+                   **{f"{x}_{s}": t.stride(i) for x, t in (("q", q), ("q_out", q), ("k", k), ("k_out", k))
+                      for i, s in ((0, "row"), (1, "head"))})
+    B.spconv_rotate_heads(a)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_odd_values_stay_in_their_head():
+    """NaN and infinities of one head reach no other; a head of zeros stays zeros."""
+    say("rotation of NaN, infinities and zeros")
+    q, k, gammas = inputs(9, 4, 2, 64, F16, seed=7, fused=False)
+    clean = B.rotate_heads(q, k, ref.ints(list(range(9))), frequencies(64), *gammas)
+    q[3, 1, 5], q[4, 2, 0], q[5, 3] = math.nan, math.inf, 0.0
+    got = B.rotate_heads(q, k, ref.ints(list(range(9))), frequencies(64), *gammas)
+    assert bool(got[0][3, 1].isnan().all()) and bool((got[0][5, 3] == 0).all()) and not bool(got[0][4, 2].isfinite().all())
+    same = torch.ones(q.shape[:2], dtype=torch.bool, device=DEV)
+    same[3, 1] = same[4, 2] = same[5, 3] = False
+    assert torch.equal(got[0][same], clean[0][same]) and torch.equal(got[1], clean[1])
+
+
+def test_no_rows():
+    q, k, _ = inputs(0, 4, 2, 64, F16)
+    got = B.rotate_heads(q, k, ref.ints([]), frequencies(64))
+    assert got[0].shape == (0, 4, 64) and got[1].shape == (0, 2, 64)
