@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libspconv.so")
 TORCH_OPS = os.path.join(HERE, "_torch_ops.so")  # the transformer operators' binding (host code only)
 SOURCES = ["api.hip", "scan.hip", "map_kernels.hip", "gmas_kernels.hip", "gemm_mfma.hip", "conv_small.hip",
            "norm.hip", "linear8.hip", "attention.hip", "attention_tile.hip", "attention_rows.hip", "attention_pages.hip",
-           "attention_pages8.hip", "rotate.hip", "cache.hip"]
+           "attention_pages8.hip", "attention_small.hip", "attention_small8.hip", "rotate.hip", "cache.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -57,10 +57,13 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
                         bool causal);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 // attention_tile.hip, attention_rows.hip: the two forms over packed keys; attention_pages.hip,
-// attention_pages8.hip: both over pages of the rows' type and of 8 bits.
+// attention_pages8.hip: both over pages of the rows' type and of 8 bits; attention_small.hip,
+// attention_small8.hip: many queries over pages of fewer rows than a wave loads at once.
 hipError_t launch_attention_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attention_rows(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attention_pages(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 hipError_t launch_attention_pages8(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attention_small(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
+hipError_t launch_attention_small8(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 
 }  // namespace spc

@@ -141,12 +141,13 @@ __device__ __forceinline__ i16x4 read_columns(const char* p) {
 // not from the sum of exponentials (131,072 keys at 2^-25.5 beside a dominant one hold 0.3 % of a
 // row).  The factor is part of both sums and leaves with their quotient.
 // 8-bit pages: half of it, as a scale's mantissa (below 2) is multiplied in before the rounding.
-template <typename T, int SRC = 0>
-constexpr float kExpRaise = !std::is_same_v<T, _Float16> ? 0.0f : SRC == 2 ? 14.0f : 15.0f;
+template <typename T, bool BITS8 = false>
+constexpr float kExpRaise = !std::is_same_v<T, _Float16> ? 0.0f : BITS8 ? 14.0f : 15.0f;
 
 // Where keys and values are: rows that follow each other; pages of the rows' type, by a table; pages
-// of 8 bits with a scale for each row.
-enum Source { kPacked = 0, kPages = 1, kPages8 = 2 };
+// of 8 bits with a scale for each row.  kSmall: pages of fewer rows than a wave loads at once.
+enum Source { kPacked, kPages, kPages8, kSmall, kSmall8 };
+constexpr bool is_bits8(int src) { return src == kPages8 || src == kSmall8; }
 
 // A document's part of the batch.
 struct Doc {
@@ -175,17 +176,17 @@ __device__ __forceinline__ Doc load_doc(const AttnArgs& a, int doc) {
 // 8-bit rows.  Keys' scales multiply the scores.  A value's scale is split: its power of two goes with
 // the conversion to 16 bits, which it leaves exact (four significant bits; float16 subnormals apart,
 // which such rows would lose in float16 pages too), and the rest, from 1 to below 2, into the
-// exponential before that is rounded.  One that is not finite stands for rows of NaN.
+// exponential before that is rounded.  One that is not finite makes its row's bytes NaN.
 struct Scale {
   float power, rest;
+  uint32_t nan;  // to be set in each four bytes
 };
 template <typename T>
 __device__ __forceinline__ Scale split_scale(float s) {
   const bool finite = s < INFINITY;
-  if constexpr (sizeof(T) == 4) return Scale{1.0f, finite ? s : NAN};
-  const uint32_t bits = __builtin_bit_cast(uint32_t, s);
-  return Scale{finite ? __builtin_bit_cast(float, bits & 0x7f800000u) : 1.0f,
-               finite ? __builtin_bit_cast(float, (bits & 0x007fffffu) | 0x3f800000u) : NAN};
+  const uint32_t bits = __builtin_bit_cast(uint32_t, finite ? s : 1.0f), nan = finite ? 0 : 0x7f7f7f7fu;
+  if constexpr (sizeof(T) == 4) return Scale{1.0f, __builtin_bit_cast(float, bits), nan};
+  return Scale{__builtin_bit_cast(float, bits & 0x7f800000u), __builtin_bit_cast(float, (bits & 0x007fffffu) | 0x3f800000u), nan};
 }
 // Eight e4m3 numbers times a power of two (16-bit types) as a fragment.
 template <typename T>

@@ -5,7 +5,10 @@
 namespace spc {
 
 hipError_t launch_attention_pages8(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
-  return p.rows ? attn::launch_rows<attn::kPages8>(a, p, dtype, s) : attn::launch_tile<attn::kPages8>(a, p, dtype, s);
+  if (p.rows) return attn::launch_rows<attn::kPages8>(a, p, dtype, s);
+  const int d = a.d <= 32 ? 32 : a.d <= 64 ? 64 : a.d <= 96 ? 96 : a.d <= 128 ? 128 : 256;
+  if (1 << a.shift < attn::rows_of_load(d, dtype == 0 ? 4 : 2, true)) return launch_attention_small8(a, p, dtype, s);
+  return attn::launch_tile<attn::kPages8>(a, p, dtype, s);
 }
 
 }  // namespace spc

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   constexpr int E = sizeof(T), ROW = lds_columns(D) * E, KT = 32;
   constexpr bool AHEAD = ROW < 1024;  // registers for the next tile while one is used
   typedef Lds<ROW> L;
-  constexpr bool BITS8 = SRC == kPages8;
+  constexpr bool BITS8 = is_bits8(SRC);
   constexpr int CB = BITS8 ? ROW / E / 16 : (int)L::CH;  // 16-byte chunks of a row of V in memory
   constexpr int P = (KT * CB + kWave - 1) / kWave;
   constexpr int STRIP = KT * ROW > D * 16 * 4 ? KT * ROW : D * 16 * 4;
@@ -190,10 +190,11 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       for (int i = 0; i < P; ++i) {
         const int p = lane + kWave * i, r = p / CB, c = p % CB;
         const float power = __shfl(mine.power, KT + r % KT);
+        const uint32_t nan = __shfl((int)mine.nan, KT + r % KT);
         if (r >= KT) continue;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const Frag f = from_e4m3<T>(rv[i][2 * j], rv[i][2 * j + 1], power);
+          const Frag f = from_e4m3<T>(rv[i][2 * j] | nan, rv[i][2 * j + 1] | nan, power);
 #pragma unroll
           for (int m = 0; m < E / 2; ++m) {
             u32x4 w;
@@ -261,15 +262,12 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
           for (int i = 0; i < 4; ++i) o[n][t][i] *= by;
         m[n] = top;
       }
-      const float off = fmaf(m[n], a.exp_by, -kExpRaise<T, SRC>);
+      const float off = fmaf(m[n], a.exp_by, -kExpRaise<T, BITS8>);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.exp_by, -off));
         l[n] += sc[i];
-        if constexpr (BITS8) {
-          const float rest = sscale[wave][1][4 * (i / 4) + g][i % 4];
-          sc[i] = masked && key(i) >= q[n].lim ? 0.0f : sc[i] * rest;
-        }
+        if constexpr (BITS8) sc[i] *= sscale[wave][1][4 * (i / 4) + g][i % 4];
       }
       fp[n] = to_frag<T>(sc);
     }

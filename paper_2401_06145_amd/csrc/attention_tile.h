@@ -43,29 +43,37 @@ __device__ __forceinline__ void bring_rows(const char* from, uint32_t bytes, cha
   }
 }
 
-// The same from an address of each lane's own: P times 16 bytes.
-template <int P>
-__device__ __forceinline__ void bring_from(const char* const* from, char* to) {
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to;
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    uint32_t kept;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, off\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(kept)
-        : "s"(__builtin_amdgcn_readfirstlane(lds + 4096 * i)), "v"(from[i])
-        : "memory");
-  }
+// The same 16 bytes a lane from an address of its own, and from one that the wave shares plus an offset.
+__device__ __forceinline__ void bring_from(const char* from, char* to) {
+  uint32_t kept;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(kept)
+      : "s"(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to)), "v"(from)
+      : "memory");
 }
-// What lanes without a row or column bring.
-__device__ __align__(16) const uint32_t kZeros[4] = {0, 0, 0, 0};
+__device__ __forceinline__ void bring_from(const char* from, uint32_t at, char* to) {
+  uint32_t kept;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(kept)
+      : "s"(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to)), "v"(at), "s"(from)
+      : "memory");
+}
+// What rows that do not exist are brought from: 16 bytes for each lane of a wave.
+__device__ __align__(16) const uint32_t kZeros[4 * kWave] = {};
 
 // Workgroups a CU holds, by the registers that rows of this many bytes need.
-constexpr int waves_a_simd(int row, int mode) {
+constexpr int waves_a_simd(int row, int mode, int src) {
+  if (is_bits8(src)) return row <= 64 ? 3 : row <= 256 ? 2 : 1;
   return row <= 64 ? (mode == kVoxel ? 3 : 4) : row <= 128 ? (mode == kVoxel ? 2 : 3) : row <= 256 ? 2 : 1;
 }
 
@@ -104,26 +112,33 @@ struct Near {
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
 // where the call is causal) start first.
 //
-// Pages: a lane looks up the pages of its rows of a tile while the tile before the last is
-// multiplied, and brings them from addresses of its own.  8 bits: rows come into registers, and are
-// widened into the other half of LDS when the tile is done, by all waves once.
+// Pages: a wave's load covers rows_of_load rows.  Pages of that many rows or more (a power of two, as all
+// are) hold them together: the page's number is looked up a tile ahead and the rows' address is the
+// wave's, by scalar instructions.  Smaller ones (kSmall): each lane looks up the page of its row and
+// computes its address (4 x 1024 queries of 16,384 keys, 32 heads of 128: 1540 us so for pages of 64).
+// 8 bits: rows come into registers, and are widened into the other half of LDS when the tile is
+// done, once for all waves.
+constexpr int rows_of_load(int d, int e, bool bits8) {
+  const int chunks = lds_columns(d) * (bits8 ? 1 : e) / 16;  // of a row
+  return chunks >= kWave ? 1 : kWave / chunks;
+}
 template <typename T, int D, int MODE, int SRC>
-__global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE, SRC)) void k_attn_tile(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
+  constexpr bool BITS8 = is_bits8(SRC), EVEN = SRC == kPages || SRC == kPages8;
   constexpr int QT = kQueryTile, E = sizeof(T), ROW = lds_columns(D) * E;
   constexpr int KT = ROW >= 1024 ? 32 : 64;
   // Rows of 256 bytes leave registers for operands ahead of their use: all of a tile of K before
   // the first product, a strip of V while the exponentials are computed (784 -> 770 us on whole
   // documents of 128 columns; with distances, or 2 strips, the registers spill; shorter
   // rows gain nothing).
-  constexpr bool AHEAD = ROW == 256 && MODE < kVoxel;
+  constexpr bool AHEAD = ROW == 256 && MODE < kVoxel && !BITS8;
   constexpr int VA = AHEAD ? 1 : 0;
   typedef Lds<ROW> L;
   // Keys between two barriers: two tiles for short rows with voxels, whose coordinates one or two
   // waves prepare while the others wait (two frames, 8 heads of 32: 169 us, so 159; of 64
   // 125, so 119; without voxels it is even, and longer rows would lose a workgroup a CU).
   constexpr int KB = MODE == kVoxel && ROW <= 128 ? 2 * KT : KT;
-  constexpr bool BITS8 = SRC == kPages8;
   constexpr int P = KB * (int)L::CH / 256;  // chunks of K (and of V) a thread brings
   constexpr int CB = BITS8 ? ROW / E / 16 : (int)L::CH;  // 16-byte chunks of a row in memory
   constexpr int PB = (KB * CB + 255) / 256;              // and of them a thread's
@@ -187,71 +202,104 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
     const int ck = L::k_chunk(r, c), cv = L::v_chunk(r, c);
     at_k[i] = ck * (16 / E) < a.d ? r * k_bytes + 16 * ck : kNowhere;
     at_v[i] = cv * (16 / E) < a.d ? r * v_bytes + 16 * cv : kNowhere;
-    if constexpr (SRC == kPages) at_k[i] = 16 * ck, at_v[i] = 16 * cv;
+    if constexpr (SRC != kPacked) at_k[i] = ck * (16 / E) < a.d ? lane / CB * (a.d * E) + 16 * ck : kNowhere,
+                                  at_v[i] = cv * (16 / E) < a.d ? lane / CB * (a.d * E) + 16 * cv : kNowhere;
   }
-  // Pages: those of this thread's rows of the tile that is brought next, and (8 bits) what it has of
-  // that tile: rows p / CB and chunks p % CB, p = threadIdx.x + 256 i.
-  int page[PB];
+  // Pages: rows RG (4 i + wave) .. of a tile are this wave's i-th, one for each CB lanes.
+  constexpr int RG = rows_of_load(D, E, BITS8);
+  int page[PB];  // of those rows of the tile that is brought next (EVEN), or of the lane's row
   u32x4 rk[BITS8 ? PB : 1], rv[BITS8 ? PB : 1];
-  float v_scale[BITS8 ? PB : 1], scale = 0.0f;
+  float k_scale[BITS8 ? PB : 1], v_scale[BITS8 ? PB : 1];
   const auto look_up = [&](int k0) {
-    if constexpr (SRC != kPacked) {
 #pragma unroll
-      for (int i = 0; i < PB; ++i) page[i] = page_at(a, doc, d, k0 + (int)(threadIdx.x + 256 * i) / CB);
+    for (int i = 0; i < PB && SRC != kPacked; ++i) {
+      const int place = k0 + RG * (4 * i + wave);
+      if constexpr (EVEN) {
+        page[i] = -1;
+        if (place < d.len_k)
+          page[i] = ((__attribute__((address_space(4))) const int32_t*)a.table)[(int64_t)doc * a.table_row + (place >> a.shift)];
+      } else {
+        page[i] = page_at(a, doc, d, place + lane / CB);
+      }
     }
+  };
+  // The first of a wave's rows (EVEN; else the lane's row) among those of its head in the pages.
+  const uint32_t page_rows = (uint32_t)a.kv_heads << a.shift;
+  if constexpr (SRC != kPacked) kp += ((int64_t)kvh << a.shift) * a.d * (BITS8 ? 1 : E), vp += ((int64_t)kvh << a.shift) * a.d * (BITS8 ? 1 : E);
+  const auto row_at = [&](int i, int place) {
+    return (uint64_t)(uint32_t)page[i] * page_rows + ((place + (EVEN ? 0 : lane / CB)) & ((1 << a.shift) - 1));
   };
   const auto bring = [&](int k0, int b) {
     if constexpr (SRC == kPacked) {
       const uint32_t rows = std::min(d.len_k - k0, KB);
       bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
       bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
-    } else if constexpr (SRC == kPages) {
-      const char *from_k[P], *from_v[P];
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const int64_t at = row_of(a, page[i], kvh, k0 + (int)(threadIdx.x + 256 * i) / CB) * (a.d * E);
-        const char* const none = reinterpret_cast<const char*>(kZeros);
-        from_k[i] = page[i] >= 0 && at_k[i] < a.d * E ? kp + at + at_k[i] : none;
-        from_v[i] = page[i] >= 0 && at_v[i] < a.d * E ? vp + at + at_v[i] : none;
-      }
-      bring_from<P>(from_k, sk[b] + 1024 * wave);
-      bring_from<P>(from_v, sv[b] + 1024 * wave);
-    } else {
+    } else if constexpr (!BITS8) {
+      const char* const none = reinterpret_cast<const char*>(kZeros);
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
-        const int p = threadIdx.x + 256 * i, r = p / CB, c = p % CB;
-        rk[i] = rv[i] = u32x4{0, 0, 0, 0};
-        v_scale[i] = 0.0f;
-        if (r >= KB || page[i] < 0) continue;
-        const int64_t row = row_of(a, page[i], kvh, k0 + r);
-        v_scale[i] = a.v_scale[row];
-        if (16 * c >= a.d) continue;
-        rk[i] = *reinterpret_cast<const u32x4*>(kp + row * a.d + 16 * c);
-        rv[i] = *reinterpret_cast<const u32x4*>(vp + row * a.d + 16 * c);
+        const int place = k0 + RG * (4 * i + wave);
+        char *const to_k = sk[b] + 1024 * (wave + 4 * i), *const to_v = sv[b] + 1024 * (wave + 4 * i);
+        const uint64_t at = row_at(i, place) * (uint32_t)(a.d * E);
+        const int have = (uint32_t)page[i] < (uint32_t)a.n_pages ? d.len_k - place : 0;  // rows from here on
+        if constexpr (EVEN) {
+          // columns that do not exist were zeros before, and stay so
+          if (have >= RG) {
+            if (at_k[i] != kNowhere) bring_from(kp + at, at_k[i], to_k);
+            if (at_v[i] != kNowhere) bring_from(vp + at, at_v[i], to_v);
+          } else if (lane / CB < have) {
+            if (at_k[i] != kNowhere) bring_from(kp + at, at_k[i], to_k);
+            if (at_v[i] != kNowhere) bring_from(vp + at, at_v[i], to_v);
+          } else {
+            bring_from(none, 16 * lane, to_k);
+            bring_from(none, 16 * lane, to_v);
+          }
+        } else {
+          const uint64_t from = at - lane / CB * (a.d * E);
+          bring_from(have > lane / CB && at_k[i] != kNowhere ? kp + from + at_k[i] : none, to_k);
+          bring_from(have > lane / CB && at_v[i] != kNowhere ? vp + from + at_v[i] : none, to_v);
+        }
       }
-      // a key's scale by one thread, a value's by another
-      static_assert(KB <= 64, "two waves");
-      scale = 0.0f;
-      const int r = threadIdx.x % 64;
-      if (threadIdx.x < 128 && r < KB) {
-        const int from = page_at(a, doc, d, k0 + r);
-        if (from >= 0) scale = (threadIdx.x < 64 ? a.k_scale : a.v_scale)[row_of(a, from, kvh, k0 + r)];
+    } else {
+      const float *const ks = a.k_scale + ((int64_t)kvh << a.shift), *const vs = a.v_scale + ((int64_t)kvh << a.shift);
+      // (columns that do not exist are others of the row: they meet zeros, and what they add goes nowhere)
+      const uint32_t r = EVEN ? lane / CB : 0, at = r * a.d + std::min(16 * (lane % CB), a.d - 16);
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+        const int first = RG * (4 * i + wave), place = k0 + first;
+        const int have = first < KB && (uint32_t)page[i] < (uint32_t)a.n_pages ? d.len_k - place : 0;
+        const uint64_t row = row_at(i, place);
+        const auto load = [&] {
+          k_scale[i] = (ks + row)[r];
+          v_scale[i] = (vs + row)[r];
+          rk[i] = *reinterpret_cast<const u32x4*>(kp + row * (uint32_t)a.d + at);
+          rv[i] = *reinterpret_cast<const u32x4*>(vp + row * (uint32_t)a.d + at);
+        };
+        if (EVEN && have >= RG) {
+          load();
+        } else {
+          rk[i] = rv[i] = u32x4{0, 0, 0, 0};
+          k_scale[i] = v_scale[i] = 0.0f;
+          if (lane / CB < have) load();
+        }
       }
     }
   };
   const auto widen = [&](int b) {
     if constexpr (BITS8) {
-      if (threadIdx.x < 128 && (int)threadIdx.x % 64 < KB)
-        reinterpret_cast<float*>(sscale[b][threadIdx.x / 64])[threadIdx.x % 64] = threadIdx.x < 64 ? scale : split_scale<T>(scale).rest;
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
-        const int p = threadIdx.x + 256 * i, r = p / CB, c = p % CB;
+        const int r = RG * (4 * i + wave) + lane / CB, c = lane % CB;
         if (KB * CB % 256 != 0 && r >= KB) continue;
-        const float power = split_scale<T>(v_scale[i]).power;
+        const Scale split = split_scale<T>(v_scale[i]);
+        if (c == 0) {
+          reinterpret_cast<float*>(sscale[b][0])[r] = k_scale[i];
+          reinterpret_cast<float*>(sscale[b][1])[r] = split.rest;
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const Frag fk = from_e4m3<T>(rk[i][2 * j], rk[i][2 * j + 1], 1.0f);
-          const Frag fv = from_e4m3<T>(rv[i][2 * j], rv[i][2 * j + 1], power);
+          const Frag fv = from_e4m3<T>(rv[i][2 * j] | split.nan, rv[i][2 * j + 1] | split.nan, split.power);
 #pragma unroll
           for (int m = 0; m < E / 2; ++m) {
             const int ch = c * E + (E / 2) * j + m;
@@ -309,6 +357,11 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
   const float vq0 = -2.0f * (half ? q.y : q.x), vq1 = half ? 1.0f : -2.0f * q.z;
   const float vq2 = fmaf(q.x, q.x, fmaf(q.y, q.y, q.z * q.z));
 
+  if (EVEN && !BITS8 && a.d * E < ROW) {
+    for (int i = threadIdx.x; i < 2 * KB * (int)L::CH; i += 256)
+      reinterpret_cast<u32x4*>(sk[0])[i] = reinterpret_cast<u32x4*>(sv[0])[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
   if (k_begin < k_end) {
     look_up(k_begin);
     bring(k_begin, 0);
@@ -394,6 +447,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = acc[i / 16][i % 16];
         if constexpr (BITS8) {
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int i = 0; i < KT / 2; ++i) s[i] *= sscale[b][0][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
         }
@@ -503,7 +557,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
             for (int i = 0; i < 16; ++i) o[t][i] *= by;
           m = top;
         }
-        const float off = fmaf(m, a.exp_by, -kExpRaise<T, SRC>);
+        const float off = fmaf(m, a.exp_by, -kExpRaise<T, BITS8>);
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.exp_by, -off));
       }
@@ -514,11 +568,9 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE)
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       if constexpr (BITS8) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < KT / 2; ++i) {
-          const float rest = sscale[b][1][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
-          s[i] = masked && key(i) >= q.lim ? 0.0f : s[i] * rest;
-        }
+        for (int i = 0; i < KT / 2; ++i) s[i] *= sscale[b][1][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
       }
       Frag fp[KT / 16];
 #pragma unroll
@@ -597,12 +649,14 @@ void tile_mode(const AttnArgs& a, hipStream_t s) {
 
 template <typename T, int SRC>
 void tile_t(const AttnArgs& a, hipStream_t s) {
-  if (a.cap == 0.0f && !a.slopes) return tile_mode<T, kBare, SRC>(a, s);
-  if constexpr (SRC == kPacked) {
-    if (a.k_pos) return tile_mode<T, kVoxel, SRC>(a, s);
-  }
-  if constexpr (!std::is_same_v<T, _Float16>) {
-    if (!a.slopes && a.cap <= kMostBoundedCap) return tile_mode<T, kCapped, SRC>(a, s);
+  if constexpr (SRC != kSmall && SRC != kSmall8) {
+    if (a.cap == 0.0f && !a.slopes) return tile_mode<T, kBare, SRC>(a, s);
+    if constexpr (SRC == kPacked) {
+      if (a.k_pos) return tile_mode<T, kVoxel, SRC>(a, s);
+    }
+    if constexpr (!std::is_same_v<T, _Float16>) {
+      if (!a.slopes && a.cap <= kMostBoundedCap) return tile_mode<T, kCapped, SRC>(a, s);
+    }
   }
   tile_mode<T, kAny, SRC>(a, s);
 }
