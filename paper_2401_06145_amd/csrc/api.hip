@@ -1154,9 +1154,9 @@ void set_cap(AttnArgs* k, float cap, float scale, bool fine) {
   k->low[1] = (float)((fit ? -0.33132737 : -1.0 / 3) * unit * by * by);
 }
 
-AttnPlan plan_of(const spconv_attention_args* a) {
+AttnPlan plan_of(const spconv_attention_args* a, bool paged = false) {
   return attention_plan(a->n_q, a->n_docs, a->max_q, a->max_k, a->heads, a->kv_heads, a->head_dim, a->dtype,
-                        a->causal != 0);
+                        a->causal != 0, paged);
 }
 
 size_t attention_bytes(const spconv_attention_args* a, const AttnPlan& p, void* base, f32x2** ml, float** o) {
@@ -1184,7 +1184,7 @@ AttnArgs attention_common(const spconv_attention_args* a, const AttnPlan& p) {
   k.exp_by = a->cap > 0.0f ? 1.0f : a->scale * kLog2e;
   // below every finite score that matters, and finite in both units
   k.floor = -3e38f / std::max(1.0f, k.exp_by);
-  k.slots = (int)p.slots, k.splits = p.splits, k.chunk = p.chunk;
+  k.slots = (int)p.slots, k.doc_slots = p.doc_slots, k.splits = p.splits, k.chunk = p.chunk;
   return k;
 }
 
@@ -1236,6 +1236,8 @@ int check_cached_attention(const spconv_pages* p, const spconv_attention_args* a
   if (p->kv_heads != a->kv_heads || p->head_dim != a->head_dim || p->n_docs != a->n_docs)
     return fail(SPCONV_EINVAL, "pages and queries differ in key heads, head_dim or documents");
   if (a->d_q_pos) return fail(SPCONV_EUNSUPPORTED, "pages hold no voxels");
+  if (a->n_q * (a->heads / a->kv_heads) > 0x7fffffff)
+    return fail(SPCONV_EUNSUPPORTED, "more than 2^31 - 1 queries of the heads of a key head");
   return SPCONV_OK;
 }
 
@@ -1325,7 +1327,7 @@ int spconv_attention(const spconv_attention_args* a, void* d_workspace, size_t w
 
 size_t spconv_cached_attention_workspace_bytes(const spconv_pages* pages, const spconv_attention_args* a) {
   if (check_cached_attention(pages, a) != SPCONV_OK) return 0;
-  return attention_bytes(a, plan_of(a), nullptr, nullptr, nullptr);
+  return attention_bytes(a, plan_of(a, true), nullptr, nullptr, nullptr);
 }
 
 int spconv_cached_attention(const spconv_pages* pages, const spconv_attention_args* a, void* d_workspace, size_t ws_bytes,
@@ -1342,7 +1344,7 @@ int spconv_cached_attention(const spconv_pages* pages, const spconv_attention_ar
     if (stride < 0 || stride * e % 16 != 0) return fail(SPCONV_EUNSUPPORTED, "strides must be multiples of 16 bytes");
   if ((a->heads > 1 && a->out_head < a->head_dim) || (a->n_q > 1 && a->out_row < a->head_dim))
     return fail(SPCONV_EINVAL, "rows or heads of d_out overlap");
-  const AttnPlan p = plan_of(a);
+  const AttnPlan p = plan_of(a, true);
   AttnArgs k = attention_common(a, p);
   const size_t need = attention_bytes(a, p, d_workspace, &k.part_ml, &k.part_o);
   if (need > 0 && (!d_workspace || ws_bytes < need)) return fail(SPCONV_ENOSPC, "attention workspace too small");

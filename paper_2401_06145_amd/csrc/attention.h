@@ -43,18 +43,20 @@ struct AttnArgs {
   const float* k_scale;  // NULL: pages hold the rows' type
   const float* v_scale;
   int paged, table_row, n_pages, shift;  // paged 0: packed keys
+  int doc_slots;  // (pages) slots of each document; 0: they go by their queries
 };
 
-// How a call runs: few queries per document (rows: their columns) or many (slots of query
-// tiles), and how its keys are split.
+// How a call runs: few queries per document (rows: their columns) or many (slots of tiles of a head's
+// queries, or of all queries of a key head's where the keys are in pages), and how its keys are split.
 struct AttnPlan {
   bool rows;
   int cols;
   int64_t slots;
+  int doc_slots;
   int splits, chunk;
 };
 AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads, int d, int dtype,
-                        bool causal);
+                        bool causal, bool paged);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s);
 // attention_tile.hip, attention_rows.hip: the two forms over packed keys; attention_pages.hip,
 // attention_pages8.hip: both over pages of the rows' type and of 8 bits; attention_small.hip,

@@ -171,14 +171,20 @@ int tile_splits(int64_t groups, int64_t rows, int max_q, int max_k, int d, bool 
 }
 
 AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads, int kv_heads, int d, int dtype,
-                        bool causal) {
+                        bool causal, bool paged) {
   AttnPlan p = {};
   const int group = heads / kv_heads;
   p.cols = (int64_t)max_q * group <= 64 ? max_q * group : 0;
   p.rows = p.cols > 0;
   // the grid's second dimension holds key heads and columns, the third the documents
   if (p.rows && (n_docs > 65535 || (int64_t)kv_heads * ((p.cols + 15) / 16) > 65535)) p.rows = false;
-  p.slots = n_q / kQueryTile + n_docs;
+  // tiles of a head's queries; over pages of all queries of a key head: a document with fewer than 128 has few rows
+  // in them (7 x 33 queries of 1501 keys, 12 heads of 80 on 4, float32: @)
+  const int64_t tile_rows = paged ? n_q * group : n_q, units = paged ? kv_heads : heads;
+  p.slots = tile_rows / kQueryTile + n_docs;
+  // as many for each document as the longest takes, where that is no more: none are empty if all are as long
+  const int64_t most = ((int64_t)max_q * group + kQueryTile - 1) / kQueryTile;
+  if (paged && most * n_docs <= p.slots) p.slots = most * n_docs, p.doc_slots = (int)most;
   int64_t splits, step;
   if (p.rows) {
     // Ranges of equal length until a launch has about 3072 workgroups (48 caches of up to 8192
@@ -190,8 +196,8 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
     splits = std::min<int64_t>((3072 + work - 1) / work, most);
     step = 128;
   } else {
-    const int64_t tiles = n_q / kQueryTile + std::min<int64_t>(n_docs, n_q);
-    splits = tile_splits(tiles * heads, n_q * heads, max_q, max_k, d, dtype == 0, causal);
+    const int64_t tiles = p.doc_slots ? p.slots : tile_rows / kQueryTile + std::min<int64_t>(n_docs, n_q);
+    splits = tile_splits(tiles * units, n_q * heads, max_q, max_k, d, dtype == 0, causal);
     step = 64;
   }
   p.chunk = (int)std::max<int64_t>(step, (((int64_t)max_k + splits - 1) / splits + step - 1) / step * step);

@@ -222,20 +222,20 @@ __device__ __forceinline__ int seen(const AttnArgs& a, const Doc& d, int i) {
   return std::min(std::max(std::max(d.len_k - d.len_q + i + 1, d.prefix), 0), d.len_k);
 }
 
-// The largest document whose first slot is at most `slot`; slots of document t start at
-// q_start[t] / tile + t, so each has room for its tiles and no running sum is needed.
-__device__ __forceinline__ int find_doc(const AttnArgs& a, int slot, int tile, int* first) {
+// The largest document whose first slot is at most `slot`; slots of document t, of `group` rows a query,
+// start at group q_start[t] / tile + t, so each has room for its tiles and no running sum is needed.
+__device__ __forceinline__ int find_doc(const AttnArgs& a, int slot, int tile, int group, int* first) {
   const int lane = threadIdx.x % kWave;
   int lo = 0, n = a.n_docs;
   while (true) {
     const int step = (n + kWave - 1) / kWave, at = lane * step;
-    const bool ok = at < n && a.q_start[lo + at] / tile + lo + at <= slot;
+    const bool ok = at < n && group * a.q_start[lo + at] / tile + lo + at <= slot;
     const int c = std::max(popc64(__ballot(ok)) - 1, 0);
     lo += c * step;
     n = std::min(step, n - c * step);
     if (step == 1) break;
   }
-  *first = a.q_start[lo] / tile + lo;
+  *first = group * a.q_start[lo] / tile + lo;
   return lo;
 }
 

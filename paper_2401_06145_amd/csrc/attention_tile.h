@@ -149,34 +149,41 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   __shared__ uint32_t odd_at[3 * KB * (D / 32)];  // NaN, +inf and -inf of a tile's values, a bit each
 
   // which slot, head and range of keys
-  const int per = a.heads * a.slots, split = blockIdx.x / per, in = blockIdx.x - split * per;
-  const int h = in % a.heads, head = a.heads % 8 == 0 ? h % 8 * (a.heads / 8) + h / 8 : h;
-  const int slot = a.slots - 1 - in / a.heads;
-  int first;
-  const int doc = find_doc(a, slot, QT, &first);
+  const int units = SRC == kPacked ? a.heads : a.kv_heads;
+  const int per = units * a.slots, split = blockIdx.x / per, in = blockIdx.x - split * per;
+  const int h = in % units, unit = units % 8 == 0 ? h % 8 * (units / 8) + h / 8 : h;
+  const int slot = a.slots - 1 - in / units;
+  // rows of the tiles: a document's queries, or (pages) theirs of all heads of a key head, next to each other
+  const int group = SRC == kPacked ? 1 : a.heads / a.kv_heads;
+  int doc, first;
+  if (SRC != kPacked && a.doc_slots) doc = slot / a.doc_slots, first = doc * a.doc_slots;
+  else doc = find_doc(a, slot, QT, group, &first);
   const Doc d = load_doc<SRC>(a, doc);
-  const int i0 = (slot - first) * QT;
-  if (i0 < 0 || i0 >= d.len_q) return;  // slots before the first document's are nobody's
-  const int kvh = head / (a.heads / a.kv_heads);
+  const int i0 = (slot - first) * QT, rows = d.len_q * group;
+  if (i0 < 0 || i0 >= rows) return;  // slots before the first document's are nobody's
+  const int kvh = SRC == kPacked ? unit / (a.heads / a.kv_heads) : unit;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = threadIdx.x % kWave, c32 = lane % 32, half = lane / 32;
 
   // the rows of this wave, and what they see
   const int row = i0 + wave * 32 + c32;
+  const int query = std::min(row, rows - 1) / group, head = SRC == kPacked ? unit : kvh * group + std::min(row, rows - 1) % group;
   const int32_t* origin = MODE == kVoxel ? a.q_pos + 4 * (int64_t)(d.q0 + i0) : nullptr;
-  const Query q = make_query(a, d, std::min(row, d.len_q - 1), head, origin);
+  const Query q = make_query(a, d, query, head, origin);
   Frag fq[D / 16];
   {
-    const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + std::min(row, d.len_q - 1)) * a.q_row + (int64_t)head * a.q_head;
+    const T* p = static_cast<const T*>(a.q) + (int64_t)(d.q0 + query) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const int at = 16 * k + 8 * half;
       fq[k] = at < a.d ? load_frag(p + at) : zero_frag<T>();
     }
   }
-  const int wave_i0 = std::min(i0 + wave * 32, d.len_q - 1);
-  const int lim_lo = seen(a, d, wave_i0), lim_hi = seen(a, d, std::min(wave_i0 + 31, d.len_q - 1));
-  const int tile_lo = seen(a, d, i0), tile_hi = seen(a, d, std::min(i0 + QT, d.len_q) - 1);
+  const int wave_i0 = std::min(i0 + wave * 32, rows - 1);
+  const int lim_lo = seen(a, d, wave_i0 / group);
+  // (pages: a wave without rows multiplies nothing)
+  const int lim_hi = SRC != kPacked && i0 + wave * 32 >= rows ? 0 : seen(a, d, std::min(wave_i0 + 31, rows - 1) / group);
+  const int tile_lo = seen(a, d, i0 / group), tile_hi = seen(a, d, (std::min(i0 + QT, rows) - 1) / group);
   const int k_begin = split * a.chunk, k_end = std::min(tile_hi, k_begin + a.chunk);
 
   f32x16 o[D / 32];
@@ -231,9 +238,9 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   };
   const auto bring = [&](int k0, int b) {
     if constexpr (SRC == kPacked) {
-      const uint32_t rows = std::min(d.len_k - k0, KB);
-      bring_rows<P>(kp + (int64_t)k0 * k_bytes, (rows - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
-      bring_rows<P>(vp + (int64_t)k0 * v_bytes, (rows - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
+      const uint32_t keys = std::min(d.len_k - k0, KB);
+      bring_rows<P>(kp + (int64_t)k0 * k_bytes, (keys - 1) * k_bytes + a.d * E, sk[b] + 1024 * wave, at_k);
+      bring_rows<P>(vp + (int64_t)k0 * v_bytes, (keys - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
     } else if constexpr (!BITS8) {
       const char* const none = reinterpret_cast<const char*>(kZeros);
 #pragma unroll
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   Near near = {0};
   bool near_q = false;
   if constexpr (MODE == kVoxel) {
-    const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + std::min(row, d.len_q - 1));
+    const int32_t* p = a.q_pos + 4 * (int64_t)(d.q0 + query);
     const uint32_t bits = ((uint32_t)p[1] - (uint32_t)origin[1]) | ((uint32_t)p[2] - (uint32_t)origin[2]) |
                           ((uint32_t)p[3] - (uint32_t)origin[3]);
     uint32_t all = 1u << 4;  // 16 is the spacing of the coarsest level
@@ -605,8 +612,8 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   }
 
   const float sum = l + __shfl_xor(l, 32);
-  if (row >= d.len_q) return;
-  const int64_t out_at = (int64_t)(d.q0 + row) * a.heads + head;
+  if (row >= rows) return;
+  const int64_t out_at = (int64_t)(d.q0 + query) * a.heads + head;
   if (a.splits > 1) {
     const int64_t part = (int64_t)split * a.n_q * a.heads + out_at;
     if (half == 0) a.part_ml[part] = f32x2{m, sum};
@@ -621,7 +628,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
       }
   } else {
     const float by = 1.0f / sum;
-    T* out = static_cast<T*>(a.out) + (int64_t)(d.q0 + row) * a.out_row + (int64_t)head * a.out_head;
+    T* out = static_cast<T*>(a.out) + (int64_t)(d.q0 + query) * a.out_row + (int64_t)head * a.out_head;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -637,7 +644,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
 
 template <typename T, int MODE, int SRC>
 void tile_mode(const AttnArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.heads * a.slots * a.splits));
+  const dim3 grid((unsigned)((int64_t)(SRC == kPacked ? a.heads : a.kv_heads) * a.slots * a.splits));
 #define SPC_D(D) hipLaunchKernelGGL((k_attn_tile<T, D, MODE, SRC>), grid, dim3(256), 0, s, a)
   if (a.d <= 32) SPC_D(32);
   else if (a.d <= 64) SPC_D(64);
@@ -663,7 +670,7 @@ void tile_t(const AttnArgs& a, hipStream_t s) {
 
 template <int SRC>
 hipError_t launch_tile(const AttnArgs& a, const AttnPlan& p, int dtype, hipStream_t s) {
-  if (!fits_launch((int64_t)a.heads * p.slots * p.splits, 256)) return hipErrorInvalidConfiguration;
+  if (!fits_launch((SRC == kPacked ? a.heads : a.kv_heads) * p.slots * p.splits, 256)) return hipErrorInvalidConfiguration;
   if (dtype == 0) tile_t<float, SRC>(a, s);
   else if (dtype == 1) tile_t<_Float16, SRC>(a, s);
   else tile_t<__bf16, SRC>(a, s);
