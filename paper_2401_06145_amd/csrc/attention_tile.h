@@ -11,8 +11,10 @@ namespace attn {
 // takes that bound for their maximum (exponentials of e^-13.2 at least), so that most tiles need
 // not look for it (whole documents 717 us; 4096 rows of 8 heads of 128 77 us, 93 with scores
 // beyond the bound, 83 and 92 by kAny, as measured in float16).  kVoxel: a bias by the
-// distance of voxels, with or without a cap.  kAny: everything else.
-enum Mode { kBare, kCapped, kVoxel, kAny };
+// distance of voxels, with or without a cap.  kPlace (pages): a bias by place and no cap; of tiles before
+// the wave's queries it is a line in the key's place, two instructions a score fewer than the
+// distance (3 x 512 float16 queries of 12,001 keys, 16 heads of 64: @).  kAny: everything else.
+enum Mode { kBare, kCapped, kVoxel, kPlace, kAny };
 constexpr float kMostBoundedCap = 60.0f;
 
 // 16 bytes a lane from memory straight into LDS, P times: those at `at[i]` of the `bytes` that
@@ -186,6 +188,10 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   const int tile_lo = seen(a, d, i0 / group), tile_hi = seen(a, d, (std::min(i0 + QT, rows) - 1) / group);
   const int k_begin = split * a.chunk, k_end = std::min(tile_hi, k_begin + a.chunk);
 
+  // kPlace: the least place of the wave's queries, and whether 2^31 places keep every slope's bias finite
+  [[maybe_unused]] const int wave_place = d.len_k - d.len_q + wave_i0 / group;
+  [[maybe_unused]] const bool even_slopes = MODE == kPlace && !__any(!(fabsf(q.slope) < 1e28f));
+
   f32x16 o[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
@@ -214,6 +220,11 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   }
   // Pages: rows RG (4 i + wave) .. of a tile are this wave's i-th, one for each CB lanes.
   constexpr int RG = rows_of_load(D, E, BITS8);
+  // A lane's row and chunk of them.  8 bits: four lanes a row and four of the next one, or the widened chunks
+  // of eight lanes, every second one of a row, would meet in the same banks of LDS.
+  constexpr bool PAIRED = BITS8 && CB >= 8;
+  const int my_row = PAIRED ? lane / (2 * CB) * 2 + lane / 4 % 2 : lane / CB;
+  const int my_chunk = PAIRED ? lane % 4 + 4 * (lane / 8 % (CB / 4)) : lane % CB;
   int page[PB];  // of those rows of the tile that is brought next (EVEN), or of the lane's row
   u32x4 rk[BITS8 ? PB : 1], rv[BITS8 ? PB : 1];
   float k_scale[BITS8 ? PB : 1], v_scale[BITS8 ? PB : 1];
@@ -226,7 +237,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
         if (place < d.len_k)
           page[i] = ((__attribute__((address_space(4))) const int32_t*)a.table)[(int64_t)doc * a.table_row + (place >> a.shift)];
       } else {
-        page[i] = page_at(a, doc, d, place + lane / CB);
+        page[i] = page_at(a, doc, d, place + my_row);
       }
     }
   };
@@ -234,7 +245,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   const uint32_t page_rows = (uint32_t)a.kv_heads << a.shift;
   if constexpr (SRC != kPacked) kp += ((int64_t)kvh << a.shift) * a.d * (BITS8 ? 1 : E), vp += ((int64_t)kvh << a.shift) * a.d * (BITS8 ? 1 : E);
   const auto row_at = [&](int i, int place) {
-    return (uint64_t)(uint32_t)page[i] * page_rows + ((place + (EVEN ? 0 : lane / CB)) & ((1 << a.shift) - 1));
+    return (uint64_t)(uint32_t)page[i] * page_rows + ((place + (EVEN ? 0 : my_row)) & ((1 << a.shift) - 1));
   };
   const auto bring = [&](int k0, int b) {
     if constexpr (SRC == kPacked) {
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
     } else {
       const float *const ks = a.k_scale + ((int64_t)kvh << a.shift), *const vs = a.v_scale + ((int64_t)kvh << a.shift);
       // (columns that do not exist are others of the row: they meet zeros, and what they add goes nowhere)
-      const uint32_t r = EVEN ? lane / CB : 0, at = r * a.d + std::min(16 * (lane % CB), a.d - 16);
+      const uint32_t r = EVEN ? my_row : 0, at = r * a.d + std::min(16 * my_chunk, a.d - 16);
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
         const int first = RG * (4 * i + wave), place = k0 + first;
@@ -287,7 +298,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
         } else {
           rk[i] = rv[i] = u32x4{0, 0, 0, 0};
           k_scale[i] = v_scale[i] = 0.0f;
-          if (lane / CB < have) load();
+          if (my_row < have) load();
         }
       }
     }
@@ -296,7 +307,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
     if constexpr (BITS8) {
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
-        const int r = RG * (4 * i + wave) + lane / CB, c = lane % CB;
+        const int r = RG * (4 * i + wave) + my_row, c = my_chunk;
         if (KB * CB % 256 != 0 && r >= KB) continue;
         const Scale split = split_scale<T>(v_scale[i]);
         if (c == 0) {
@@ -417,12 +428,27 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
       const int sub = (k0 - kb) / KT;
       const char *const tk = sk[b] + sub * KT * ROW, *const tv = sv[b] + sub * KT * ROW;
       float s[KT / 2];
+      const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
+      const auto key = [&](int i) { return k0 + at(i); };
+      // kPlace: the scores begin with their bias
+      [[maybe_unused]] float bias[MODE == kPlace ? KT / 2 : 1];
+      if constexpr (MODE == kPlace) {
+        if (even_slopes && k0 + KT <= wave_place) {
+          const float first = q.slope * (float)(k0 + 4 * half - q.place);
+#pragma unroll
+          for (int i = 0; i < KT / 2; ++i) bias[i] = fmaf(q.slope, (float)(at(i) - 4 * half), first);
+        } else {
+#pragma unroll
+          for (int i = 0; i < KT / 2; ++i) bias[i] = 0.0f;
+          add_place_bias<KT / 2>(q, bias, key);
+        }
+      }
       {
         f32x16 acc[KT / 32];
 #pragma unroll
         for (int h = 0; h < KT / 32; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[h][i] = 0.0f;
+          for (int i = 0; i < 16; ++i) acc[h][i] = MODE == kPlace && !BITS8 ? bias[16 * h + i] : 0.0f;
         const auto key_rows = [&](int h, int k) {
           const int r = 32 * h + c32;
           if constexpr (E == 4) {
@@ -456,7 +482,10 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
         if constexpr (BITS8) {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int i = 0; i < KT / 2; ++i) s[i] *= sscale[b][0][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
+          for (int i = 0; i < KT / 2; ++i) {
+            const float by = sscale[b][0][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
+            s[i] = MODE == kPlace ? fmaf(s[i], by, bias[i]) : s[i] * by;
+          }
         }
       }
       // columns of V: fragment (t, c) of out^T's rows 32 t .. and keys 16 c + {4 half + j, 8 + 4 half + j}
@@ -490,8 +519,6 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
       }
 
       const bool masked = k0 + KT > lim_lo;
-      const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
-      const auto key = [&](int i) { return k0 + at(i); };
       if constexpr (MODE == kCapped) {
         float most = 0.0f;
 #pragma unroll
@@ -527,7 +554,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
       } else {
-        if (MODE != kBare && a.cap > 0.0f) cap_scores<KT / 2, E == 4>(a, s);
+        if (MODE != kBare && MODE != kPlace && a.cap > 0.0f) cap_scores<KT / 2, E == 4>(a, s);
         if constexpr (MODE == kVoxel) {
           if (near_q && snear[b][sub]) {
 #pragma unroll
@@ -663,6 +690,9 @@ void tile_t(const AttnArgs& a, hipStream_t s) {
     }
     if constexpr (!std::is_same_v<T, _Float16>) {
       if (!a.slopes && a.cap <= kMostBoundedCap) return tile_mode<T, kCapped, SRC>(a, s);
+    }
+    if constexpr (SRC != kPacked) {
+      if (a.cap == 0.0f) return tile_mode<T, kPlace, SRC>(a, s);
     }
   }
   tile_mode<T, kAny, SRC>(a, s);
