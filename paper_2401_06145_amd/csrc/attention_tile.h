@@ -225,6 +225,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
   constexpr bool PAIRED = BITS8 && CB >= 8;
   const int my_row = PAIRED ? lane / (2 * CB) * 2 + lane / 4 % 2 : lane / CB;
   const int my_chunk = PAIRED ? lane % 4 + 4 * (lane / 8 % (CB / 4)) : lane % CB;
+  const bool whole = EVEN && 1 << a.shift >= KB;  // a tile lies in one page
   int page[PB];  // of those rows of the tile that is brought next (EVEN), or of the lane's row
   u32x4 rk[BITS8 ? PB : 1], rv[BITS8 ? PB : 1];
   float k_scale[BITS8 ? PB : 1], v_scale[BITS8 ? PB : 1];
@@ -233,6 +234,10 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
     for (int i = 0; i < PB && SRC != kPacked; ++i) {
       const int place = k0 + RG * (4 * i + wave);
       if constexpr (EVEN) {
+        if (i > 0 && whole) {
+          page[i] = page[0];
+          continue;
+        }
         page[i] = -1;
         if (place < d.len_k)
           page[i] = ((__attribute__((address_space(4))) const int32_t*)a.table)[(int64_t)doc * a.table_row + (place >> a.shift)];
@@ -254,6 +259,16 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
       bring_rows<P>(vp + (int64_t)k0 * v_bytes, (keys - 1) * v_bytes + a.d * E, sv[b] + 1024 * wave, at_v);
     } else if constexpr (!BITS8) {
       const char* const none = reinterpret_cast<const char*>(kZeros);
+      if (whole && k0 + KB <= d.len_k && (uint32_t)page[0] < (uint32_t)a.n_pages) {
+        const uint64_t at = row_at(0, k0 + RG * wave) * (uint32_t)(a.d * E);
+        const char *from_k = kp + at, *from_v = vp + at;
+#pragma unroll
+        for (int i = 0; i < PB; ++i, from_k += 4 * RG * a.d * E, from_v += 4 * RG * a.d * E) {
+          if (at_k[i] != kNowhere) bring_from(from_k, at_k[i], sk[b] + 1024 * (wave + 4 * i));
+          if (at_v[i] != kNowhere) bring_from(from_v, at_v[i], sv[b] + 1024 * (wave + 4 * i));
+        }
+        return;
+      }
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
         const int place = k0 + RG * (4 * i + wave);
@@ -480,7 +495,6 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = acc[i / 16][i % 16];
         if constexpr (BITS8) {
-          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int i = 0; i < KT / 2; ++i) {
             const float by = sscale[b][0][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
@@ -602,7 +616,6 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       if constexpr (BITS8) {
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] *= sscale[b][1][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
       }
