@@ -417,9 +417,9 @@ int spconv_rotate_heads(const spconv_rotation* args, void* stream);
  * with an infinity gets an infinite scale and stands for NaN; scales that the caller writes are
  * at least 2^-126).  Else they hold rows of the calls' `dtype`.
  * page is a power of two up to 65536, head_dim a multiple of 8 (8 bits: of 16) up to 256, pages
- * 16-byte aligned, table_row * page at most 2^30.  Entries of the table that no key of a call
- * needs are not read; one outside [0, n_pages) is never followed: nothing is written there, and its
- * keys and values are zeros. */
+ * 16-byte aligned, table_row * page at most 2^30, a page's keys at most 2^29 elements.  Entries of the table
+ * that no key of a call needs may be anything; one outside [0, n_pages) is never followed: nothing is
+ * written there, and its keys and values are zeros. */
 typedef struct {
   void* d_k; /* [n_pages][kv_heads][page][head_dim] */
   void* d_v;

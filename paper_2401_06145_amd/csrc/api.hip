@@ -1205,6 +1205,8 @@ int check_pages(const spconv_pages* p, int dtype, int64_t n) {
     return fail(SPCONV_EUNSUPPORTED, "head_dim must be a multiple of 8 (8-bit pages: of 16) up to 256");
   if (p->page < 1 || p->page > kMostPage || (p->page & (p->page - 1)) != 0)
     return fail(SPCONV_EUNSUPPORTED, "rows of a page must be a power of two up to 65536");
+  if ((int64_t)p->kv_heads * p->page * p->head_dim > 1 << 29)  // (offsets inside a page have 32 bits, in bytes)
+    return fail(SPCONV_EUNSUPPORTED, "more than 2^29 elements in a page of keys");
   if ((int64_t)p->table_row * p->page > 1 << 30) return fail(SPCONV_EUNSUPPORTED, "more than 2^30 keys in a document");
   if (n == 0 || p->n_docs == 0) return SPCONV_OK;
   if ((p->n_pages > 0 && (!p->d_k || !p->d_v)) || (p->table_row > 0 && !p->d_table)) return fail(SPCONV_EINVAL, "NULL pointer");

@@ -179,7 +179,7 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
   // the grid's second dimension holds key heads and columns, the third the documents
   if (p.rows && (n_docs > 65535 || (int64_t)kv_heads * ((p.cols + 15) / 16) > 65535)) p.rows = false;
   // tiles of a head's queries; over pages of all queries of a key head: a document with fewer than 128 has few rows
-  // in them (7 x 33 queries of 1501 keys, 12 heads of 80 on 4, float32: @)
+  // in them (7 x 33 queries of 1501 keys, 12 heads of 80 on 4, float32: 86 us, so 36 with slots without gaps)
   const int64_t tile_rows = paged ? n_q * group : n_q, units = paged ? kv_heads : heads;
   p.slots = tile_rows / kQueryTile + n_docs;
   // as many for each document as the longest takes, where that is no more: none are empty if all are as long
@@ -193,7 +193,10 @@ AttnPlan attention_plan(int64_t n_q, int n_docs, int max_q, int max_k, int heads
     // four ranges, 9.2 by eight; 2048 by 16 even; 300 keys 6.7 by one, 7.7 by two).
     const int64_t work = std::max<int64_t>((int64_t)n_docs * kv_heads, 1);
     const int most = max_k < 512 ? 1 : std::max(max_k / 256, std::min(kFewRanges, max_k / 128));
-    splits = std::min<int64_t>((3072 + work - 1) / work, most);
+    // Over pages about 1536, which begin with a chain of loads more (one token for each of 48 documents of up to
+    // 2048 keys, 32 heads of 128 on 8: 8 bits 50 us with 3072, 44 so, the rows' type 69 and 62; of 8
+    // documents of 16,384 75 and 67, 120 and 110; of 48 up to 8192 145 and 143, 226 and 229).
+    splits = std::min<int64_t>(((paged ? 1536 : 3072) + work - 1) / work, most);
     step = 128;
   } else {
     const int64_t tiles = p.doc_slots ? p.slots : tile_rows / kQueryTile + std::min<int64_t>(n_docs, n_q);

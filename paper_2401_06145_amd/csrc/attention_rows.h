@@ -32,6 +32,11 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   constexpr bool AHEAD = ROW < 1024;  // registers for the next tile while one is used
   typedef Lds<ROW> L;
   constexpr bool BITS8 = is_bits8(SRC);
+  // Tiles on their way beside the one in use: two of 8 bits, which take half of the registers (one token for
+  // each of 48 documents of up to 8192 keys, 32 heads of 128 on 8: 150 us with one).
+  constexpr int DEPTH = BITS8 && NC == 1 && ROW <= 256 ? 2 : 1;
+  typedef std::integral_constant<int, 0> Set0;
+  typedef std::integral_constant<int, DEPTH - 1> Set1;
   constexpr int CB = BITS8 ? ROW / E / 16 : (int)L::CH;  // 16-byte chunks of a row of V in memory
   constexpr int P = (KT * CB + kWave - 1) / kWave;
   constexpr int STRIP = KT * ROW > D * 16 * 4 ? KT * ROW : D * 16 * 4;
@@ -44,6 +49,18 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   // XCDs would get the ranges that only long documents fill (8 ranges of 48 caches: 219 us, so 160).
   const int doc = blockIdx.z, kvh = blockIdx.y % a.kv_heads, col0 = blockIdx.y / a.kv_heads * 16 * NC;
   const int split = (blockIdx.x + doc + kvh) % a.splits;
+  // Pages: the first ones are looked up beside the document's lengths, and may be none of its.
+  const int k_begin = split * a.chunk, k_first = k_begin + (int)threadIdx.x / kWave * KT;
+  const auto entry = [&](int place) {
+    place += threadIdx.x % KT;
+    if (place >= 0 && place >> a.shift < a.table_row) return a.table[(int64_t)doc * a.table_row + (place >> a.shift)];
+    return -1;
+  };
+  [[maybe_unused]] int first_page = -1, second_page = -1;
+  if constexpr (SRC != kPacked) {
+    first_page = entry(k_first);
+    if constexpr (DEPTH == 2) second_page = entry(k_first + 4 * KT);
+  }
   const Doc d = load_doc<SRC>(a, doc);
   const int group = a.heads / a.kv_heads, cols = d.len_q * group;
   if (cols <= col0) return;
@@ -70,7 +87,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
   }
   const int lim_lo = seen(a, d, 0), lim_hi = seen(a, d, d.len_q - 1);
-  const int k_begin = split * a.chunk, k_end = std::min(lim_hi, k_begin + a.chunk);
+  const int k_end = std::min(lim_hi, k_begin + a.chunk);
 
   f32x4 o[NC][D / 16];
   float m[NC], l[NC];
@@ -84,20 +101,31 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   const T* kp = static_cast<const T*>(a.k);
   const T* vp = static_cast<const T*>(a.v);
   if constexpr (SRC == kPacked) kp += d.k0 * a.k_row + (int64_t)kvh * a.k_head, vp += d.k0 * a.v_row + (int64_t)kvh * a.v_head;
+  // Pages: this head's part of the first one, and the way to the next.  A row's address is one product of
+  // 32 bits and a sum.
+  constexpr int B = BITS8 ? 1 : E;  // bytes of an element
+  const uint32_t row_bytes = a.d * B, page_rows = (uint32_t)a.kv_heads << a.shift, page_bytes = page_rows * row_bytes;
+  const int64_t head_rows = (int64_t)kvh << a.shift;
+  const char *const kb = static_cast<const char*>(a.k) + head_rows * row_bytes, *const vb = static_cast<const char*>(a.v) + head_rows * row_bytes;
+  const auto offset = [&](int page, int place) {
+    return (uint64_t)(uint32_t)page * page_bytes + (uint32_t)((place & ((1 << a.shift) - 1)) * row_bytes);
+  };
 
   // A tile's operands: K's rows as the product takes them (8 bits: as they lie), V's as they lie, the
   // voxels of the first KT lanes.  Their registers take the next tile as soon as they are used, so that
   // its loads are under way for the rest of the work on this one.
   Frag fk[2][BITS8 ? 1 : D / 32];
-  u32x4 rk[2][BITS8 ? (D / 32 + 1) / 2 : 1];
-  u32x4 rv[P];
-  float scale = 0.0f;  // of K's rows in the first KT lanes, of V's in the others
+  u32x4 rk[DEPTH][2][BITS8 ? (D / 32 + 1) / 2 : 1];
+  u32x4 rv[DEPTH][P];
+  float scale[DEPTH] = {};  // of K's rows in the first KT lanes, of V's in the others
   int page = -1;       // of key lane % KT of the tile whose rows are loaded next
   int32_t pos[4] = {0, 0, 0, 0};
   const auto fetch_pages = [&](int k0) {
     if constexpr (SRC != kPacked) page = page_at(a, doc, d, k0 + lane % KT);
   };
-  const auto fetch_k = [&](int k0) {
+  const auto checked = [&](int of, int k0) { return k0 + lane % KT < d.len_k && (uint32_t)of < (uint32_t)a.n_pages ? of : -1; };
+  const auto fetch_k = [&](int k0, auto set) {
+    constexpr int S = decltype(set)::value;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = 16 * h + c16, key = k0 + r;
@@ -110,68 +138,75 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         }
       } else {
         const int from = __shfl(page, r);
-        const int64_t row = row_of(a, from, kvh, key) * a.d;
+        const char* p = kb + offset(from, key);
         if constexpr (!BITS8) {
 #pragma unroll
           for (int k = 0; k < D / 32; ++k) {
             const int at = 32 * k + 8 * g;
-            fk[h][k] = from >= 0 && at < a.d ? load_frag(kp + row + at) : zero_frag<T>();
+            fk[h][k] = from >= 0 && at < a.d ? load_frag(reinterpret_cast<const T*>(p) + at) : zero_frag<T>();
           }
         } else {
-          const char* p = static_cast<const char*>(a.k) + row;
 #pragma unroll
           for (int k = 0; k < (D / 32 + 1) / 2; ++k) {
             const int at = col_of(2 * k);
-            rk[h][k] = u32x4{0, 0, 0, 0};
+            rk[S][h][k] = u32x4{0, 0, 0, 0};
             if (from < 0 || at >= a.d) continue;
             if (2 * k + 1 < D / 32) {
-              rk[h][k] = *reinterpret_cast<const u32x4*>(p + at);
+              rk[S][h][k] = *reinterpret_cast<const u32x4*>(p + at);
             } else {
               const u32x2 w = *reinterpret_cast<const u32x2*>(p + at);
-              rk[h][k] = u32x4{w[0], w[1], 0, 0};
+              rk[S][h][k] = u32x4{w[0], w[1], 0, 0};
             }
           }
         }
       }
     }
   };
-  const auto fetch_v = [&](int k0) {
+  const auto fetch_v = [&](int k0, auto set) {
+    constexpr int S = decltype(set)::value;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int p = lane + kWave * i, r = p / CB, c = p % CB;
-      rv[i] = u32x4{0, 0, 0, 0};
+      rv[S][i] = u32x4{0, 0, 0, 0};
       if constexpr (SRC == kPacked) {
         if (k0 + r < d.len_k && c * (16 / E) < a.d)
-          rv[i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
+          rv[S][i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(k0 + r) * a.v_row + c * (16 / E));
       } else {
         const int from = __shfl(page, r % KT);
-        if (r < KT && from >= 0 && c * (BITS8 ? 16 : 16 / E) < a.d)
-          rv[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.v) + row_of(a, from, kvh, k0 + r) * a.d * (BITS8 ? 1 : E) + 16 * c);
+        if (r < KT && from >= 0 && c * (16 / B) < a.d) rv[S][i] = *reinterpret_cast<const u32x4*>(vb + offset(from, k0 + r) + 16 * c);
       }
     }
     if constexpr (BITS8) {
-      scale = 0.0f;
-      if (page >= 0) scale = (lane < KT ? a.k_scale : a.v_scale)[row_of(a, page, kvh, k0 + lane % KT)];
+      scale[S] = 0.0f;
+      if (page >= 0)
+        scale[S] = ((lane < KT ? a.k_scale : a.v_scale) + head_rows)[(uint64_t)(uint32_t)page * page_rows + ((k0 + lane % KT) & ((1 << a.shift) - 1))];
     }
     if (SRC == kPacked && a.k_pos && lane < KT && k0 + lane < d.len_k) {
 #pragma unroll
       for (int i = 1; i < 4; ++i) pos[i] = a.k_pos[4 * (d.k0 + k0 + lane) + i];
     }
   };
-  const int k_first = k_begin + wave * KT;
-  fetch_pages(k_first);
+  if constexpr (SRC != kPacked) page = checked(first_page, k_first);
   if (AHEAD && k_first < k_end) {
-    fetch_v(k_first);
-    fetch_k(k_first);
-    fetch_pages(k_first + 4 * KT);
+    fetch_v(k_first, Set0());
+    fetch_k(k_first, Set0());
+    if constexpr (DEPTH == 2) {
+      page = checked(second_page, k_first + 4 * KT);
+      if (k_first + 4 * KT < k_end) {
+        fetch_v(k_first + 4 * KT, Set1());
+        fetch_k(k_first + 4 * KT, Set1());
+      }
+    }
+    fetch_pages(k_first + 4 * DEPTH * KT);
   }
-  for (int k0 = k_first; k0 < k_end; k0 += 4 * KT) {
+  const auto tile = [&](int k0, auto set) {
+    constexpr int S = decltype(set)::value;
     const bool masked = k0 + KT > lim_lo;
-    if (!AHEAD) fetch_v(k0);
+    if (!AHEAD) fetch_v(k0, set);
     bool bad = false;
     if (masked && !BITS8) {
 #pragma unroll
-      for (int i = 0; i < P; ++i) bad |= odd_values<T>(rv[i]);
+      for (int i = 0; i < P; ++i) bad |= odd_values<T>(rv[S][i]);
     }
     if (SRC == kPacked && a.k_pos && lane < KT) {  // keys that do not exist are hidden, wherever they are
       const Voxel v = voxel_from(pos, origin);
@@ -181,11 +216,11 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int p = lane + kWave * i, r = p / CB, c = p % CB;
-        *reinterpret_cast<u32x4*>(sv + r * ROW + 16 * L::v_chunk16(r, c)) = rv[i];
+        *reinterpret_cast<u32x4*>(sv + r * ROW + 16 * L::v_chunk16(r, c)) = rv[S][i];
       }
     } else {
-      const Scale mine = split_scale<T>(scale);
-      reinterpret_cast<float*>(sscale[wave])[lane] = lane < KT ? scale : mine.rest;
+      const Scale mine = split_scale<T>(scale[S]);
+      reinterpret_cast<float*>(sscale[wave])[lane] = lane < KT ? scale[S] : mine.rest;
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int p = lane + kWave * i, r = p / CB, c = p % CB;
@@ -194,7 +229,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         if (r >= KT) continue;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const Frag f = from_e4m3<T>(rv[i][2 * j] | nan, rv[i][2 * j + 1] | nan, power);
+          const Frag f = from_e4m3<T>(rv[S][i][2 * j] | nan, rv[S][i][2 * j + 1] | nan, power);
 #pragma unroll
           for (int m = 0; m < E / 2; ++m) {
             u32x4 w;
@@ -205,9 +240,10 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         }
       }
     }
-    const bool more = AHEAD && k0 + 4 * KT < k_end;
-    if (!AHEAD) fetch_k(k0);
-    if (more) fetch_v(k0 + 4 * KT);
+    const int next = k0 + 4 * DEPTH * KT;
+    const bool more = AHEAD && next < k_end;
+    if (!AHEAD) fetch_k(k0, set);
+    if (more) fetch_v(next, set);
     const bool careful = masked && __any(bad);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -220,13 +256,13 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         s[n][h] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
-          if constexpr (BITS8) s[n][h] = Mat<T>::mma16(from_e4m3<T>(rk[h][k / 2][2 * (k % 2)], rk[h][k / 2][2 * (k % 2) + 1], 1.0f), fq[n][k], s[n][h]);
+          if constexpr (BITS8) s[n][h] = Mat<T>::mma16(from_e4m3<T>(rk[S][h][k / 2][2 * (k % 2)], rk[S][h][k / 2][2 * (k % 2) + 1], 1.0f), fq[n][k], s[n][h]);
           else s[n][h] = Mat<T>::mma16(fk[h][k], fq[n][k], s[n][h]);
         }
       }
     if (more) {
-      fetch_k(k0 + 4 * KT);
-      fetch_pages(k0 + 8 * KT);
+      fetch_k(next, set);
+      fetch_pages(next + 4 * KT);
     } else if (!AHEAD) {
       fetch_pages(k0 + 4 * KT);
     }
@@ -320,6 +356,10 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+  };
+  for (int k0 = k_first; k0 < k_end; k0 += 4 * DEPTH * KT) {
+    tile(k0, Set0());
+    if (DEPTH == 2 && k0 + 4 * KT < k_end) tile(k0 + 4 * KT, Set1());
   }
 
   // join of the four waves
