@@ -14,13 +14,21 @@ are part of the norms):
 ``forward`` runs whole documents: voxels that all see each other, nearer ones counting more
 (``causal=False`` with coordinates), or a scene's tokens as a prefix that all see, with text after
 it that sees backwards.  ``prefill`` and ``step`` are the same with caches: a batch's prompts, then
-one new token for each document a call.
+one new token for each document a call.  ``extend`` is for documents that come and go and grow by any
+number of tokens a call, prompts in chunks and single tokens together: their caches are pages, in the
+rows' type or in 8 bits.
+
+Between the first product and attention, where the configuration asks for it:
+
+  q, k = norm of each head, turned by their places or voxels    spconv_rotate_heads
+  pages <- k, v                                                 spconv_cache_write
+  o     = attention(q, pages)                                   spconv_cached_attention
 
     python -m paper_2401_06145_amd.transformer      # a small UNet encoder, its voxels, ten new tokens
 """
 from __future__ import annotations
 
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 
 import torch
 
@@ -37,6 +45,11 @@ class Config:
     cap: float = 30.0     # of the scores; 0: none
     eps: float = 1e-6
     exact: bool = False   # products summed in float32 throughout (spconv_scaled_linear's exact), at about half the rate
+    head_norm: bool = False   # norms of queries and keys for each head
+    rotary: int = 0           # columns of a head that turn by place, or by the voxel's coordinates; 0: none
+    base: float = 10_000.0    # of the frequencies
+    factor: float = 1.0       # for contexts that many times longer than ``trained`` (binding.rotary_frequencies)
+    trained: int = 0
 
     @property
     def head_dim(self) -> int:
@@ -53,6 +66,60 @@ class Caches:
     prefix: torch.Tensor | None
     room: int
     longest: int           # the longest length, known to the host
+
+
+@dataclass
+class PagedCaches:
+    """Keys and values of each layer in pages that all documents share out among them; the same table for
+    every layer.  Lengths are known to the host, which gives pages out as documents grow."""
+    layers: list              # of B.Pages
+    table: torch.Tensor       # int32 [docs][most pages of one]
+    length: torch.Tensor      # int32 [docs]
+    lens: list                # the same, on the host
+    free: list                # pages of no document
+    dtype: torch.dtype
+    prefix: torch.Tensor | None = None
+    held: list = field(default_factory=list)  # pages of each document, in order
+
+    @property
+    def page(self) -> int:
+        return self.layers[0].page
+
+    def grow(self, new: list) -> None:
+        """Room for new[t] more tokens of each document t; all of it or, where pages run out, none."""
+        if len(new) != len(self.lens) or any(n < 0 for n in new):
+            raise ValueError(f"expected {len(self.lens)} numbers of new tokens, got {new}")
+        lens = [a + b for a, b in zip(self.lens, new)]
+        more = [-(-n // self.page) - len(p) for n, p in zip(lens, self.held)]
+        if max(lens, default=0) > self.table.shape[1] * self.page:
+            raise ValueError(f"a document of {max(lens)} tokens does not fit {self.table.shape[1]} pages of {self.page}")
+        if sum(more) > len(self.free):
+            raise ValueError(f"{sum(more)} more pages are needed, and {len(self.free)} are free")
+        at, of = [], []
+        for t, m in enumerate(more):
+            for _ in range(m):
+                at.append(t * self.table.shape[1] + len(self.held[t]))
+                of.append(self.free.pop())
+                self.held[t].append(of[-1])
+        if at:
+            both = torch.tensor([at, of], dtype=torch.int64).to(self.table.device)
+            self.table.view(-1)[both[0]] = both[1].to(torch.int32)
+        self.lens = lens
+        self.length += torch.tensor(new, dtype=torch.int32).to(self.length.device)
+
+    def release(self, doc: int) -> None:
+        """Document ``doc`` ends: its pages are free, and its place is an empty document's."""
+        self.free.extend(reversed(self.held[doc]))
+        self.held[doc], self.lens[doc] = [], 0
+        self.length[doc] = 0
+        if self.prefix is not None:
+            self.prefix[doc] = 0
+
+    def read(self, layer: int) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(keys, values, first row of each document) of one layer, packed as ``attention`` takes them."""
+        start = torch.tensor([sum(self.lens[:t]) for t in range(len(self.lens) + 1)], dtype=torch.int32).to(self.table.device)
+        k, v = B.cache_read(self.layers[layer], start, self.table, sum(self.lens), self.dtype)
+        return k, v, start
 
 
 def documents(coords: torch.Tensor) -> tuple[torch.Tensor, int]:
@@ -83,13 +150,26 @@ class Transformer:
                             up=weight(c.inner, c.width), down=weight(c.width, c.inner), g_in=gamma(c.width),
                             g_out=gamma(c.width), g_up=gamma(c.width), g_down=gamma(c.inner)) for _ in range(c.layers)]
         self.g_last = gamma(c.width)
+        if c.head_norm:
+            for w in self.layers:
+                w["g_q"], w["g_k"] = gamma(c.head_dim), gamma(c.head_dim)
+        self.freq, self.gain = B.rotary_frequencies(c.rotary, c.base, c.factor, c.trained, device=self.device)
         self.slopes = torch.exp2(-8.0 * torch.arange(1, c.heads + 1) / c.heads).to(self.device)
 
     def _linear(self, rows, weight, relu=False):
         return B.scaled_linear(rows[0], rows[1], weight[0], weight[1], self.dtype, relu=relu, exact=self.config.exact)
 
-    def _run(self, x: torch.Tensor, attend) -> torch.Tensor:
-        """The layers on rows x; attend(layer, q, k, v) is their attention."""
+    def _places(self, n: int, start: torch.Tensor, first: torch.Tensor | None = None) -> torch.Tensor | None:
+        """Each of n rows' place in its document, whose rows begin at place ``first`` (0)."""
+        if not (self.config.rotary or self.config.head_norm):
+            return None
+        row = torch.arange(n, device=self.device)
+        doc = torch.searchsorted(start[1:].contiguous(), row, right=True).clamp(max=len(start) - 2)
+        place = row - start[doc]
+        return (place if first is None else place + first[doc]).to(torch.int32)
+
+    def _run(self, x: torch.Tensor, attend, pos: torch.Tensor | None = None) -> torch.Tensor:
+        """The layers on rows x; attend(layer, q, k, v) is their attention; pos: the rows' places or voxels."""
         c = self.config
         kv = c.kv_heads * c.head_dim
         add = None
@@ -97,6 +177,8 @@ class Transformer:
             *a, total = B.rms_norm(x, w["g_in"], residual=add, eps=c.eps, bits8=True)
             x = x if add is None else total
             q, k, v = (t.unflatten(1, (-1, c.head_dim)) for t in self._linear(a, w["qkv"]).split([c.width, kv, kv], 1))
+            if c.rotary or c.head_norm:
+                q, k = B.rotate_heads(q, k, pos, self.freq, w.get("g_q"), w.get("g_k"), eps=c.eps, gain=self.gain)
             o = attend(i, q, k, v).flatten(1)
             add = self._linear(B.rms_norm(o, w["g_out"], eps=c.eps, bits8=True)[:2], w["out"])
             *a, x = B.rms_norm(x, w["g_up"], residual=add, eps=c.eps, bits8=True)
@@ -107,11 +189,12 @@ class Transformer:
     def forward(self, x: torch.Tensor, start: torch.Tensor, longest: int, coords: torch.Tensor | None = None,
                 causal: bool = False, prefix: torch.Tensor | None = None, spacing: int = 1) -> torch.Tensor:
         """Whole documents: rows x [n][width], document t being rows start[t] .. start[t + 1].  With
-        coords, scores fall with the voxels' distance, in units of ``spacing`` (the level's)."""
+        coords, scores fall with the voxels' distance, in units of ``spacing`` (the level's), and heads
+        turn, if they do, by the voxels' coordinates."""
         slopes = None if coords is None else self.slopes / spacing
         return self._run(x, lambda i, q, k, v: B.attention(
             q, k, v, start, start, longest, longest, prefix=prefix, causal=causal, cap=self.config.cap, slopes=slopes,
-            q_pos=coords, k_pos=coords))
+            q_pos=coords, k_pos=coords), self._places(len(x), start) if coords is None else coords)
 
     def prefill(self, x: torch.Tensor, start: torch.Tensor, longest: int, room: int,
                 prefix: torch.Tensor | None = None) -> tuple[torch.Tensor, Caches]:
@@ -133,7 +216,7 @@ class Transformer:
                 kept[-1][at] = new
             return B.attention(q, k, v, start, start, longest, longest, prefix=prefix, causal=True, cap=c.cap)
 
-        return self._run(x, attend), caches
+        return self._run(x, attend, self._places(len(x), start)), caches
 
     def step(self, x: torch.Tensor, caches: Caches) -> torch.Tensor:
         """One new token for each document: rows x [docs][width]; the caches grow by one key."""
@@ -150,7 +233,32 @@ class Transformer:
             return B.attention(q, caches.k[i], caches.v[i], one, caches.start, 1, caches.longest, k_len=caches.length,
                                prefix=caches.prefix, causal=True, cap=self.config.cap)
 
-        return self._run(x, attend)
+        return self._run(x, attend, (caches.length - 1).contiguous())
+
+    def pages(self, docs: int, pages: int, page: int = 64, bits8: bool = False, most: int | None = None,
+              prefix: torch.Tensor | None = None) -> PagedCaches:
+        """Caches of ``pages`` pages a layer for ``docs`` documents, empty ones, of up to ``most`` pages each."""
+        c = self.config
+        return PagedCaches([B.Pages.make(pages, page, c.kv_heads, c.head_dim, self.dtype, bits8, self.device) for _ in range(c.layers)],
+                           torch.full((docs, most or pages), -1, dtype=torch.int32, device=self.device),
+                           torch.zeros(docs, dtype=torch.int32, device=self.device), [0] * docs, list(range(pages))[::-1],
+                           self.dtype, None if prefix is None else prefix.clone(), [[] for _ in range(docs)])
+
+    def extend(self, x: torch.Tensor, new: list, caches: PagedCaches) -> torch.Tensor:
+        """New tokens for each document, any number (a prompt, its next chunk, one token, none): rows
+        x [sum(new)][width] in the documents' order; the caches grow by them."""
+        if len(x) != sum(new):
+            raise ValueError(f"{sum(new)} new tokens, but {len(x)} rows")
+        first = caches.length.clone()
+        caches.grow(new)
+        start = torch.tensor([sum(new[:t]) for t in range(len(new) + 1)], dtype=torch.int32).to(self.device)
+
+        def attend(i, q, k, v):
+            B.cache_write(caches.layers[i], k, v, start, caches.length, caches.table)
+            return B.cached_attention(q, caches.layers[i], start, caches.length, caches.table, max(new), max(caches.lens),
+                                      prefix=caches.prefix, cap=self.config.cap)
+
+        return self._run(x, attend, self._places(len(x), start, first)) if len(x) else x
 
 
 def main() -> None:
@@ -171,7 +279,21 @@ def main() -> None:
     x = torch.randn((len(length), tokens.shape[1]), device=dev).to(torch.bfloat16)
     for _ in range(10):
         x = model.step(x, caches)
+    # the same scenes, turned by place, as documents in 8-bit pages: a chunk of voxels at a time, then new tokens
+    turned = Transformer(Config(width=tokens.shape[1], head_norm=True, rotary=tokens.shape[1] // 8))
+    lens = length.tolist()
+    paged = turned.pages(len(lens), sum(-(-(n + 10) // 64) for n in lens), bits8=True)
+    for at in range(0, longest, 1024):
+        chunk = [max(0, min(1024, n - at)) for n in lens]
+        rows = torch.cat([tokens[int(start[t]) + at:int(start[t]) + at + n] for t, n in enumerate(chunk)])
+        y = turned.extend(rows, chunk, paged)
+    y = torch.randn((len(lens), tokens.shape[1]), device=dev).to(torch.bfloat16)
+    for _ in range(10):
+        y = turned.extend(y, [1] * len(lens), paged)
+    keys, _, _ = paged.read(0)
     torch.cuda.synchronize()
+    print(f"in pages: {len(keys)} keys a layer, rms {float(keys.float().square().mean().sqrt()):.3f}; "
+          f"rms of the last tokens {float(y.float().square().mean().sqrt()):.3f}")
     print(f"{len(cloud)} voxels, {len(coords)} tokens in {len(length)} scenes, 10 new tokens each; "
           f"rms of the last {float(x.float().square().mean().sqrt()):.3f}")
 
