@@ -392,7 +392,8 @@ int spconv_attention(const spconv_attention_args* args, void* d_workspace, size_
  *   d_q_out, d_k_out  the same shapes; may be d_q and d_k with the same strides, and overlap them
  *               in no other way.
  *   d_q_gamma, d_k_gamma  [head_dim] in `dtype`, each NULL for no norm.
- * head_dim 1 to 256, rotated even and at most head_dim (0: the norm alone; d_pos and d_freq unused). */
+ * head_dim 1 to 256, rotated even and at most head_dim (0: the norm alone; d_pos and d_freq unused);
+ * rows up to what one launch takes (2^32 threads, 256 for at most 16 rows: SPCONV_EUNSUPPORTED beyond). */
 typedef struct {
   const void* d_q;
   void* d_q_out;
@@ -435,7 +436,8 @@ typedef struct {
  * it goes to place k_len[t] - (q_start[t + 1] - q_start[t]) + i.  Rows of no document, and places
  * before 0 or behind the table, are left out.  d_k, d_v: rows n, kv_heads, head_dim in `dtype`, 16-byte
  * aligned, strides multiples of 16 bytes.  Two rows for one place (documents that share a page)
- * leave either's elements. */
+ * leave either's elements.  Rows up to what one launch takes (2^32 threads, 256 for at most 64 rows:
+ * SPCONV_EUNSUPPORTED beyond), here and in spconv_cache_read. */
 int spconv_cache_write(const spconv_pages* pages, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
                        int64_t v_row, int64_t v_head, const int32_t* d_q_start, const int32_t* d_k_len, int64_t n,
                        int dtype, void* stream);
@@ -451,7 +453,9 @@ int spconv_cache_read(const spconv_pages* pages, void* d_k, int64_t k_row, int64
  * d_k, d_v, their strides, d_k_start and n_k are not used, d_k_len has to be given, and voxels are
  * not supported; n_docs, kv_heads and head_dim are those of the pages.  The rest is as there: its
  * masks, prefix, cap, bias by place, rows that stay as they are, and limits.  8-bit rows count as
- * the exact values that they stand for, except in float16 where those are subnormal. */
+ * the exact values that they stand for, except with float16 queries where those are beyond that
+ * type's range or subnormal in it.  More than 2^31 - 1 rows of queries times heads of a key head:
+ * SPCONV_EUNSUPPORTED. */
 size_t spconv_cached_attention_workspace_bytes(const spconv_pages* pages, const spconv_attention_args* args);
 int spconv_cached_attention(const spconv_pages* pages, const spconv_attention_args* args, void* d_workspace,
                             size_t ws_bytes, void* stream);

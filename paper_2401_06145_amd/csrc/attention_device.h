@@ -144,6 +144,12 @@ __device__ __forceinline__ i16x4 read_columns(const char* p) {
 template <typename T, bool BITS8 = false>
 constexpr float kExpRaise = !std::is_same_v<T, _Float16> ? 0.0f : BITS8 ? 14.0f : 15.0f;
 
+// An exponential's argument is the score times exp_by less that of the maximum, in one instruction; the
+// latter's rounding is the same for all scores of a row, and leaves with the quotient.  From maxima of 2^31 on
+// it would be more than float32's range of exponents: over pages, larger ones than this are
+// subtracted first.  (Over packed keys slopes of some 1e9 and more give NaN.)
+constexpr float kMostOffset = 0x1p20f;
+
 // Where keys and values are: rows that follow each other; pages of the rows' type, by a table; pages
 // of 8 bits with a scale for each row.  kSmall: pages of fewer rows than a wave loads at once.
 enum Source { kPacked, kPages, kPages8, kSmall, kSmall8 };

@@ -13,7 +13,7 @@ namespace attn {
 // beyond the bound, 83 and 92 by kAny, as measured in float16).  kVoxel: a bias by the
 // distance of voxels, with or without a cap.  kPlace (pages): a bias by place and no cap; of tiles before
 // the wave's queries it is a line in the key's place, two instructions a score fewer than the
-// distance (3 x 512 float16 queries of 12,001 keys, 16 heads of 64: @).  kAny: everything else.
+// distance (3 x 512 float16 queries of 12,001 keys, 16 heads of 64: 141 us, so 125).  kAny: everything else.
 enum Mode { kBare, kCapped, kVoxel, kPlace, kAny };
 constexpr float kMostBoundedCap = 60.0f;
 
@@ -114,12 +114,14 @@ struct Near {
 // the 8 XCDs), so that its L2 serves K and V; the longest rows (the last of a document,
 // where the call is causal) start first.
 //
-// Pages: a wave's load covers rows_of_load rows.  Pages of that many rows or more (a power of two, as all
+// Pages: a tile's rows are the queries of all heads of a key head, next to each other.  A wave's load covers rows_of_load rows.  Pages of that many rows or more (a power of two, as all
 // are) hold them together: the page's number is looked up a tile ahead and the rows' address is the
 // wave's, by scalar instructions.  Smaller ones (kSmall): each lane looks up the page of its row and
 // computes its address (4 x 1024 queries of 16,384 keys, 32 heads of 128: 1540 us so for pages of 64).
 // 8 bits: rows come into registers, and are widened into the other half of LDS when the tile is
-// done, once for all waves.
+// done, once for all waves.  4 x 1024 queries of up to 16,384 keys, 32 heads of 128 on 8, bfloat16: packed keys
+// 1085 us, pages 1134 (0.94 PFLOP/s), 8 bits 1360 (0.78): two products a score, its scales from LDS and the
+// widening are 60 % more vector instructions, and the waves wait for LDS.
 constexpr int rows_of_load(int d, int e, bool bits8) {
   const int chunks = lds_columns(d) * (bits8 ? 1 : e) / 16;  // of a row
   return chunks >= kWave ? 1 : kWave / chunks;
@@ -605,7 +607,12 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
             for (int i = 0; i < 16; ++i) o[t][i] *= by;
           m = top;
         }
-        const float off = fmaf(m, a.exp_by, -kExpRaise<T, BITS8>);
+        float off = fmaf(m, a.exp_by, -kExpRaise<T, BITS8>);
+        if (SRC != kPacked && __any(fabsf(off) > kMostOffset && m > a.floor)) {
+          off = -kExpRaise<T, BITS8>;
+#pragma unroll
+          for (int i = 0; i < KT / 2; ++i) s[i] -= m;
+        }
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.exp_by, -off));
       }

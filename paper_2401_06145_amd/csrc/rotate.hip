@@ -8,7 +8,8 @@
 // heads; then a group of lanes takes a head, and a lane both columns of its pairs, so that a head is
 // read once and nothing is exchanged but the sum of squares.  Angles are products of float64,
 // of which whole turns are taken off before they become float32: at place 10^6 a float32 angle would
-// be off by 0.06.  What bounds it is memory.
+// be off by 0.06.  What bounds it is memory: 65,536 rows of 40 heads of 128 in bfloat16, 1.34 GB,
+// 266 us (5.0 TB/s, what a large copy reaches); for one row the host's call (5.4 us, the kernel 2.5).
 #include <algorithm>
 
 #include "rotate.h"

@@ -197,3 +197,21 @@ def test_binding_refuses_what_needs_gradients():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="GPU|device"):
             call()
+
+
+@pytest.mark.parametrize("call", [
+    lambda: rotation(n=(1 << 31) - 1), lambda: rotation(n=(1 << 31) - 1, heads=65535, kv_heads=0),
+    lambda: write(pages(), n=(1 << 31) - 1), lambda: read(pages(kv_heads=64), n=(1 << 31) - 1, k_row=4096, v_row=4096),
+    lambda: attend(pages(n_docs=1 << 24), n_q=1 << 24, n_docs=1 << 24, max_q=40, heads=2, max_k=9),
+    lambda: attend(pages(n_docs=1 << 26), n_q=70, n_docs=1 << 26, max_q=40, max_k=9),
+])
+def test_more_than_one_launch_takes(call):
+    """2^32 threads and more would start as fewer, without an error."""
+    assert call() == B.SPCONV_EUNSUPPORTED
+    assert b"launch" in B.lib().spconv_last_error()
+
+
+def test_queries_of_a_key_head_have_31_bits():
+    assert attend(pages(kv_heads=1), n_q=1 << 30, kv_heads=1, max_q=1 << 30) == B.SPCONV_EUNSUPPORTED
+    assert B.spconv_cached_attention_workspace_bytes(pages(kv_heads=1), attention_args(n_q=1 << 30, kv_heads=1, max_q=1 << 30)) == 0
+    assert write(pages(kv_heads=1 << 12, page=1 << 16, head_dim=64, table_row=1)) == B.SPCONV_EUNSUPPORTED

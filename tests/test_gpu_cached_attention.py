@@ -256,3 +256,62 @@ def test_strided_queries():
     wide = torch.randn((63, 8, 64), device=DEV).to(BF16)
     wide[:, 2:6] = b.q
     assert torch.equal(b.run(q=wide[:, 2:6]), b.run())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bits8", [False, True])
+def test_slopes_of_all_sizes(bits8, dtype):
+    """A bias by place of any size, also far from the queries."""
+    say(f"slopes of all sizes over pages, 8 bits {bits8} {dtype}")
+    for ql, kl in (([3, 1], [700, 90]), ([150, 70], [200, 3000])):
+        b = Cached(ql, kl, 8, 2, 64, dtype, bits8, 32, seed=13)
+        slopes = torch.tensor([0.0, 1e-6, 1e-3, 1.0, -1e-2, 1e20, 1e37, math.inf], device=DEV)
+        got = b.run(slopes=slopes)
+        assert bool(got[:, 7].isnan().all())  # infinity times the distance 0
+        want, mag = b.want(slopes=slopes)
+        check_attention(got[:, :7], want[:, :7], mag[:, :7], "finite slopes")
+        for causal, prefix in ((False, None), (True, [n // 2 for n in kl])):
+            got = b.run(slopes=slopes[:7].repeat(2)[:8].contiguous(), causal=causal, prefix=prefix)
+            want, mag = b.want(slopes=slopes[:7].repeat(2)[:8], causal=causal, prefix=prefix)
+            check_attention(got, want, mag, f"causal {causal}, prefix {prefix}")
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 16, 32, 64, 128, 1024])
+def test_pages_of_all_sizes(page, bits8):
+    """Pages that end inside a tile, hold many tiles, or one row; every width."""
+    say(f"attention over pages of {page}, 8 bits {bits8}")
+    for d in (16, 32, 64, 96, 128, 256):
+        for ql, kl, dtype in (([70, 1, 200], [77, 300, 517], BF16), ([1, 2], [517, 64], F32), ([65], [129], F32)):
+            b = Cached(ql, kl, 2, 1, d, dtype, bits8, page, seed=page + d)
+            check_attention(b.run(), *b.want(), f"{d} columns, {ql} of {kl}, {dtype}")
+            check_attention(b.run(cap=15.0, prefix=[n // 3 for n in kl]), *b.want(cap=15.0, prefix=[n // 3 for n in kl]), "capped")
+
+
+def test_lengths_at_the_ends_of_tiles():
+    """Every length around the ends of pages, tiles and ranges."""
+    say("attention over pages, lengths from 1 to 260")
+    for ql in (1, 40):
+        for dtype, bits8 in ((BF16, True), (F16, False), (F32, True)):
+            kl = [n for n in range(1, 261) if min(n % 16, -n % 16) <= 1]
+            b = Cached([min(ql, n) for n in kl], kl, 4, 2, 32, dtype, bits8, 16, seed=14)
+            check_attention(b.run(), *b.want(), f"{ql} queries {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("size", [1e4, 1e9, 1e14])
+def test_scores_of_all_sizes(size, bits8, dtype):
+    """Scores far beyond what exponentials take: the largest wins, wherever it is, whatever its sign."""
+    say(f"scores of {size} over pages, 8 bits {bits8} {dtype}")
+    for ql, kl in (([3, 1], [700, 90]), ([150], [400])):
+        b = Cached(ql, kl, 4, 2, 64, dtype, bits8, 32, seed=16)
+        towards = torch.sign(torch.randn(64, device=DEV))
+        for sign in (1.0, -1.0):
+            # keys i (2 + i) / 1024 along one direction, apart by more than any rounding of the scores
+            k = torch.cat([(2 + torch.arange(n, device=DEV).flip(0)) / 1024 for n in kl])[:, None, None] * towards
+            c = Cached(ql, kl, 4, 2, 64, dtype, bits8, 32, seed=16, like=(k.expand(-1, 2, -1).contiguous(), torch.randn((sum(kl), 2, 64), device=DEV)))
+            c.q[:] = (sign * size * towards).to(dtype)
+            got, (want, mag) = c.run(scale=1.0, causal=False), c.want(scale=1.0, causal=False)
+            # 8-bit keys share values, 16-bit ones some: where two largest are equal both count
+            check_attention(got, want, mag, f"{sign}")
