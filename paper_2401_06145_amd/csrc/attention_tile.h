@@ -74,7 +74,8 @@ __device__ __forceinline__ void bring_from(const char* from, uint32_t at, char* 
 __device__ __align__(16) const uint32_t kZeros[4 * kWave] = {};
 
 // Workgroups a CU holds, by the registers that rows of this many bytes need.
-constexpr int waves_a_simd(int row, int mode, int src) {
+constexpr int waves_a_simd(int row, int mode, int src, int e) {
+  if (src != kPacked && e == 4 && row == 512) return 2;
   if (is_bits8(src)) return row <= 64 ? 3 : row <= 256 ? 2 : 1;
   return row <= 64 ? (mode == kVoxel ? 3 : 4) : row <= 128 ? (mode == kVoxel ? 2 : 3) : row <= 256 ? 2 : 1;
 }
@@ -127,11 +128,11 @@ constexpr int rows_of_load(int d, int e, bool bits8) {
   return chunks >= kWave ? 1 : kWave / chunks;
 }
 template <typename T, int D, int MODE, int SRC>
-__global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE, SRC)) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE, SRC, sizeof(T))) void k_attn_tile(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
   constexpr bool BITS8 = is_bits8(SRC), EVEN = SRC == kPages || SRC == kPages8;
   constexpr int QT = kQueryTile, E = sizeof(T), ROW = lds_columns(D) * E;
-  constexpr int KT = ROW >= 1024 ? 32 : 64;
+  constexpr int KT = ROW >= 1024 || (SRC != kPacked && E == 4 && ROW == 512) ? 32 : 64;
   // Rows of 256 bytes leave registers for operands ahead of their use: all of a tile of K before
   // the first product, a strip of V while the exponentials are computed (784 -> 770 us on whole
   // documents of 128 columns; with distances, or 2 strips, the registers spill; shorter

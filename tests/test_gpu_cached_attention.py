@@ -46,12 +46,16 @@ def test_documents(case, bits8, dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("case", [1, 3, 9, 10, 12])
 def test_as_over_packed_keys(case, dtype):
-    """The same keys packed: the same kernels but for where a row comes from, and the same bits."""
+    """The same keys packed: the same kernels but for where a row comes from, and the same bits; float32 rows of
+    more than 64 columns go through tiles of half the keys, so that sums have another order."""
     ql, kl, heads, kv, d, page = (FEW + MANY)[case]
     say(f"attention over pages and packed keys {ql} of {kl} {dtype}")
     b = Cached(ql, kl, heads, kv, d, dtype, False, page, seed=case)
     packed = B.attention(b.q, b.k.to(dtype), b.v.to(dtype), b.q_start, cref.starts(kl), max(ql), max(kl), causal=True)
-    assert torch.equal(b.run(), packed)
+    if dtype != F32 or d <= 64:
+        assert torch.equal(b.run(), packed)
+    else:
+        check_attention(b.run(), packed.double(), b.want()[1], "pages and packed keys")
 
 
 @pytest.mark.parametrize("dtype", TYPES)
