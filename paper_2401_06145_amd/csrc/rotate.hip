@@ -11,6 +11,7 @@
 // be off by 0.06.  What bounds it is memory: 65,536 rows of 40 heads of 128 in bfloat16, 1.34 GB,
 // 266 us (5.0 TB/s, what a large copy reaches); for one row the host's call (5.4 us, the kernel 2.5).
 #include <algorithm>
+#include <type_traits>
 
 #include "rotate.h"
 
@@ -85,6 +86,20 @@ __device__ __forceinline__ Part part_of(int i, int d, int rot) {
   return Part{c < d ? c : -1, c + W < d ? c + W : -1, false};
 }
 
+// Cosines and sines of the pairs of a workgroup's rows, [rows][rot / 2] each.
+__device__ __forceinline__ void turns_of(const RotateArgs& a, int64_t row0, int rows, float* cosines, float* sines) {
+  const int half = a.rot / 2;
+  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+    const int r = i / half, j = i - r * half;
+    const int32_t p = a.voxels ? a.pos[4 * (row0 + r) + 1 + j % 3] : a.pos[row0 + r];
+    const double turns = p * (a.freq[j] * 0.15915494309189535);
+    float s, c;
+    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    cosines[i] = a.gain * c;
+    sines[i] = a.gain * s;
+  }
+}
+
 // G lanes a head, I parts of two runs of W columns a lane.
 template <typename T, int W, int I, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, int g) {
@@ -121,15 +136,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, int g) {
   int t = threadIdx.x / g;
   if (t < tasks) fetch(t);
 
-  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
-    const int r = i / half, j = i - r * half;
-    const int32_t p = a.voxels ? a.pos[4 * (row0 + r) + 1 + j % 3] : a.pos[row0 + r];
-    const double turns = p * (a.freq[j] * 0.15915494309189535);
-    float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-    cosines[r * half + j] = a.gain * c;
-    sines[r * half + j] = a.gain * s;
-  }
+  turns_of(a, row0, rows, cosines, sines);
   __syncthreads();
 
   for (; t < tasks; t += groups) {
@@ -201,6 +208,97 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, int g) {
   }
 }
 
+// Heads whose pairs or addresses fit no wide access (an odd width, an odd number of pairs): rows of
+// heads that follow each other come through LDS in 16-byte pieces, and go back so; a lane has single pairs of
+// a head, as above with W = 1.  From 2^23 elements on (41,323 rows of 20 heads of 33, 32 turned, bfloat16: element by
+// element from memory 175 us, 109 so; 6724 rows of 24 heads of 256, 50 turned, float16 110 and 90; but 2539
+// rows of 24 heads of 33 11.1 and 12.3).  Bound by the vector unit and LDS, a few instructions an element.
+constexpr int kStage = 4096;  // elements
+template <typename T, int I, bool INTER>
+__global__ __launch_bounds__(kThreads) void k_rotate_staged(RotateArgs a, int g, int tile_rows) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float cosines[kMostRows * kMostRotated / 2], sines[kMostRows * kMostRotated / 2];
+  __shared__ __align__(16) T stage[kStage + 16];
+  const int half = a.rot / 2, heads = a.heads[0] + a.heads[1];
+  const int64_t row0 = (int64_t)blockIdx.x * a.per;
+  const int rows = (int)std::min<int64_t>(a.per, a.n - row0);
+  const int groups = kThreads / g, lane = threadIdx.x % g;
+  Part part[I];
+#pragma unroll
+  for (int i = 0; i < I; ++i) part[i] = part_of<1, INTER>(lane + g * i, a.d, a.rot);
+  turns_of(a, row0, rows, cosines, sines);
+
+  for (int r0 = 0; r0 < rows; r0 += tile_rows)
+    for (int h0 = 0; h0 < heads; h0 += a.share) {
+      const int nr = std::min(tile_rows, rows - r0), nh = std::min(a.share, heads - h0);
+      // of the tile's heads, those of the queries and of the keys; each begins at 16 bytes
+      const int of[2] = {std::max(0, std::min(nh, a.heads[0] - h0)), nh - std::max(0, std::min(nh, a.heads[0] - h0))};
+      const int off = (of[0] * a.d + 7) / 8 * 8, pitch = off + (of[1] * a.d + 7) / 8 * 8;
+      const auto copy = [&](auto out) {
+        constexpr bool OUT = decltype(out)::value;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int n = of[k] * a.d, first = k ? std::max(0, h0 - a.heads[0]) : h0;
+          if (n == 0) continue;
+          const int64_t ld = OUT ? a.y_row[k] : a.x_row[k];
+          T* const base = (OUT ? static_cast<T*>(a.y[k]) : const_cast<T*>(static_cast<const T*>(a.x[k]))) + (row0 + r0) * ld + (int64_t)first * a.d;
+          T* const here = stage + (k ? off : 0);
+          const bool wide = reinterpret_cast<uintptr_t>(base) % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0;
+          const int pieces = wide ? n / V : 0, rest = n - pieces * V;
+          for (int i = threadIdx.x; i < nr * pieces; i += kThreads) {
+            const int r = i / pieces, c = (i - r * pieces) * V;
+            u32x4 *const l = reinterpret_cast<u32x4*>(here + r * pitch + c), *const m = reinterpret_cast<u32x4*>(base + r * ld + c);
+            if (OUT) *m = *l;
+            else *l = *m;
+          }
+          for (int i = threadIdx.x; i < nr * rest; i += kThreads) {
+            const int r = i / rest, c = pieces * V + i - r * rest;
+            if (OUT) base[r * ld + c] = here[r * pitch + c];
+            else here[r * pitch + c] = base[r * ld + c];
+          }
+        }
+      };
+      copy(std::false_type());
+      __syncthreads();
+      for (int t = threadIdx.x / g; t < nr * nh; t += groups) {
+        const int r = t / nh, h = t - r * nh, k = h >= of[0];
+        T* const x = stage + r * pitch + (k ? off + (h - of[0]) * a.d : h * a.d);
+        float v[I][2];
+        float sq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+          v[i][0] = part[i].ca >= 0 ? (float)x[part[i].ca] : 0.0f;
+          v[i][1] = part[i].cb >= 0 ? (float)x[part[i].cb] : 0.0f;
+          sq = fmaf(v[i][0], v[i][0], fmaf(v[i][1], v[i][1], sq));
+        }
+        if (a.gamma[k]) {
+          for (int m = 1; m < g; m *= 2) sq += __shfl_xor(sq, m);
+          const float inv = 1.0f / sqrtf(sq / (float)a.d + a.eps);
+          const T* gamma = static_cast<const T*>(a.gamma[k]);
+#pragma unroll
+          for (int i = 0; i < I; ++i) {
+            if (part[i].ca >= 0) v[i][0] *= inv * (float)gamma[part[i].ca];
+            if (part[i].cb >= 0) v[i][1] *= inv * (float)gamma[part[i].cb];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+          if (part[i].turned) {
+            const int j = (r0 + r) * half + (INTER ? part[i].ca / 2 : part[i].ca);
+            const float p = v[i][0], q = v[i][1], co = cosines[j], si = sines[j];
+            v[i][0] = p * co - q * si;
+            v[i][1] = p * si + q * co;
+          }
+          if (part[i].ca >= 0) x[part[i].ca] = (T)v[i][0];
+          if (part[i].cb >= 0) x[part[i].cb] = (T)v[i][1];
+        }
+      }
+      __syncthreads();
+      copy(std::true_type());
+      __syncthreads();
+    }
+}
+
 template <typename T, bool INTER>
 hipError_t rotate_t(RotateArgs a, hipStream_t s) {
   // the widest runs of columns that pairs and all addresses allow
@@ -225,6 +323,18 @@ hipError_t rotate_t(RotateArgs a, hipStream_t s) {
   a.share = heads;
   // few rows: a workgroup for as many heads as it has groups
   if (a.n < 1024) a.share = std::min(heads, groups);
+  bool follow = true;  // heads of every row
+  for (int k = 0; k < 2; ++k) follow = follow && (a.heads[k] <= 1 || (a.x_head[k] == a.d && a.y_head[k] == a.d));
+  if (w == 1 && follow && a.n * heads * a.d >= 1 << 23) {
+    a.share = std::min(heads, kStage / a.d / 8 * 8);
+    const int tile_rows = a.share < heads ? 1 : std::max(1, std::min(kMostRows, kStage / (heads * a.d + 16)));
+    a.per = (int)std::min<int64_t>({std::max(4, tile_rows), std::max<int64_t>(1, a.n / 1024), kMostRows});
+    const int64_t wgs = (a.n + a.per - 1) / a.per;
+    if (!fits_launch(wgs, kThreads)) return hipErrorInvalidConfiguration;
+    if (parts <= kWave) hipLaunchKernelGGL((k_rotate_staged<T, 1, INTER>), dim3((unsigned)wgs), dim3(kThreads), 0, s, a, g, tile_rows);
+    else hipLaunchKernelGGL((k_rotate_staged<T, 2, INTER>), dim3((unsigned)wgs), dim3(kThreads), 0, s, a, g, tile_rows);
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)((a.n + a.per - 1) / a.per), (unsigned)((heads + a.share - 1) / a.share));
   if (!fits_launch((a.n + a.per - 1) / a.per, kThreads) || grid.y > 65535) return hipErrorInvalidConfiguration;
   if (w == 8) hipLaunchKernelGGL((k_rotate<T, 8, 1, INTER>), grid, dim3(kThreads), 0, s, a, g);

@@ -131,3 +131,25 @@ def test_no_rows():
     q, k, _ = inputs(0, 4, 2, 64, F16)
     got = B.rotate_heads(q, k, ref.ints([]), frequencies(64))
     assert got[0].shape == (0, 4, 64) and got[1].shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,rot,hq,hkv", [(33, 32, 7, 3), (256, 50, 13, 3), (255, 254, 9, 30), (20, 6, 40, 0), (7, 6, 300, 301)])
+def test_many_rows_of_widths_that_fit_no_wide_access(d, rot, hq, hkv, dtype):
+    """From 2^23 elements on they go through LDS: rows of q and k apart by any stride, the last rows few."""
+    n = (1 << 23) // ((hq + hkv) * d) + 37
+    say(f"rotation of {n} rows, {hq} + {hkv} heads of {d}, {rot} turned, {dtype}")
+    g = torch.Generator(DEV).manual_seed(d)
+    pos = torch.arange(n, device=DEV, dtype=torch.int32) - 100
+    for first, interleaved, normed in ((0, False, True), (3, True, False)):
+        wide = torch.randn((n, (hq + hkv) * d + 5), device=DEV, generator=g).to(dtype)
+        q = wide[:, first:first + hq * d].unflatten(1, (hq, d))
+        k = wide[:, first + hq * d:first + (hq + hkv) * d].unflatten(1, (hkv, d)) if hkv else None
+        gammas = [(1 + 0.2 * torch.randn(d, device=DEV, generator=g)).to(dtype) if normed else None for _ in range(2)]
+        got = B.rotate_heads(q, k, pos, frequencies(rot), *gammas, interleaved=interleaved)
+        rows = torch.cat([torch.arange(200, device=DEV), torch.arange(n - 200, n, device=DEV),
+                          torch.randint(0, n, (400,), device=DEV, generator=g)])
+        for x, y, gamma in ((q, got[0], gammas[0]), (k, got[1], gammas[1])):
+            if x is not None:
+                ref.check_rotated(y[rows], *ref.rotate(x[rows], pos[rows], frequencies(rot), gamma, interleaved=interleaved),
+                                  f"from column {first}")
