@@ -218,10 +218,6 @@ __device__ __forceinline__ int page_at(const AttnArgs& a, int doc, const Doc& d,
   const int page = a.table[(int64_t)doc * a.table_row + (place >> a.shift)];
   return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
 }
-// The row of a head's part of that page, among all rows of the pages.
-__device__ __forceinline__ int64_t row_of(const AttnArgs& a, int page, int kvh, int place) {
-  return (((int64_t)page * a.kv_heads + kvh) << a.shift) + (place & ((1 << a.shift) - 1));
-}
 // Number of keys that query i sees: the first ones of its document.
 __device__ __forceinline__ int seen(const AttnArgs& a, const Doc& d, int i) {
   if (!a.causal) return d.len_k;
