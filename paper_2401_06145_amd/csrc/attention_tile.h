@@ -425,6 +425,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
         __syncthreads();
         for (uint32_t p = threadIdx.x; p < KB * L::CH; p += 256) {
           const int r = p / L::CH, x = L::v_chunk(r, p % L::CH) * (16 / E);
+          if (x >= D) continue;  // no product takes these (rows of 96 columns; of 8 bits they repeat the row's last)
           for (int j = 0; j < 16 / E; ++j) {
             T* v = reinterpret_cast<T*>(sv[b] + 16 * p) + j;
             const int kind = odd_kind((float)*v);
