@@ -144,11 +144,13 @@ __device__ __forceinline__ i16x4 read_columns(const char* p) {
 template <typename T, bool BITS8 = false>
 constexpr float kExpRaise = !std::is_same_v<T, _Float16> ? 0.0f : BITS8 ? 14.0f : 15.0f;
 
-// An exponential's argument is the score times exp_by less that of the maximum, in one instruction; the
-// latter's rounding is the same for all scores of a row, and leaves with the quotient.  From maxima of 2^31 on
-// it would be more than float32's range of exponents: over pages, larger ones than this are
-// subtracted first.  (Over packed keys slopes of some 1e9 and more give NaN.)
-constexpr float kMostOffset = 0x1p20f;
+// An exponential's argument is the score times exp_by less that of the maximum, in one instruction.  The
+// latter product is rounded.  Its error is a factor of all exponentials of one maximum, which leaves with their
+// quotient; but a row's tiles, waves and key ranges have maxima of their own, and are joined by their exact
+// differences.  Maxima up to this size weigh parts wrongly by 2^-17 + 2^-17 in units of log2, 1.1e-5, at
+// most; larger ones are subtracted first, which is exact near the maximum (scores of 1000, maxima apart by up to 2: 7e-5
+// without that, of 500,000 4 %, and NaN from 2^31 on).
+constexpr float kMostOffset = 0x1p8f;
 
 // Where keys and values are: rows that follow each other; pages of the rows' type, by a table; pages
 // of 8 bits with a scale for each row.  kSmall: pages of fewer rows than a wave loads at once.

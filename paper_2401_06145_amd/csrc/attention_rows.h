@@ -300,10 +300,12 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         m[n] = top;
       }
       float off = fmaf(m[n], a.exp_by, -kExpRaise<T, BITS8>);
-      if (SRC != kPacked && __any(fabsf(off) > kMostOffset && m[n] > a.floor)) {
-        off = -kExpRaise<T, BITS8>;
+      const bool large = fabsf(off) > kMostOffset;
+      if (__any(large)) {  // (of this row: others keep their bits)
+        const float first = large ? m[n] : 0.0f;
+        off = large ? -kExpRaise<T, BITS8> : off;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sc[i] -= m[n];
+        for (int i = 0; i < 8; ++i) sc[i] -= first;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -610,10 +610,12 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
           m = top;
         }
         float off = fmaf(m, a.exp_by, -kExpRaise<T, BITS8>);
-        if (SRC != kPacked && __any(fabsf(off) > kMostOffset && m > a.floor)) {
-          off = -kExpRaise<T, BITS8>;
+        const bool large = fabsf(off) > kMostOffset;
+        if (__any(large)) {  // (of this row: others keep their bits)
+          const float first = large ? m : 0.0f;
+          off = large ? -kExpRaise<T, BITS8> : off;
 #pragma unroll
-          for (int i = 0; i < KT / 2; ++i) s[i] -= m;
+          for (int i = 0; i < KT / 2; ++i) s[i] -= first;
         }
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.exp_by, -off));
