@@ -11,8 +11,8 @@ namespace attn {
 // takes that bound for their maximum (exponentials of e^-13.2 at least), so that most tiles need
 // not look for it (whole documents 717 us; 4096 rows of 8 heads of 128 77 us, 93 with scores
 // beyond the bound, 83 and 92 by kAny, as measured in float16).  kVoxel: a bias by the
-// distance of voxels, with or without a cap.  kPlace (pages): a bias by place and no cap; of tiles before
-// the wave's queries it is a line in the key's place, two instructions a score fewer than the
+// distance of voxels, with or without a cap.  kPlace (pages): a bias by place and no cap; in tiles before
+// or behind the wave's queries it is a line in the key's place, two instructions a score fewer than the
 // distance (3 x 512 float16 queries of 12,001 keys, 16 heads of 64: 141 us, so 125).  kAny: everything else.
 enum Mode { kBare, kCapped, kVoxel, kPlace, kAny };
 constexpr float kMostBoundedCap = 60.0f;
@@ -449,13 +449,18 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
       float s[KT / 2];
       const auto at = [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * half + i % 4; };
       const auto key = [&](int i) { return k0 + at(i); };
-      // kPlace: the scores begin with their bias
-      [[maybe_unused]] float bias[MODE == kPlace ? KT / 2 : 1];
+      // kPlace: the sums begin with the bias less that of the tile's first key, a line of at most 63 slopes; the
+      // first key's, which is as large as the document is long, joins the maximum.  (Sums that began with
+      // all of it would round each of their steps at its size, which shows where far keys count: negative slopes.)
+      // Tiles beside the queries' own places have small distances, and begin with all of theirs.
+      [[maybe_unused]] float bias[MODE == kPlace ? KT / 2 : 1], bias0 = 0.0f;
       if constexpr (MODE == kPlace) {
-        if (even_slopes && k0 + KT <= wave_place) {
-          const float first = q.slope * (float)(k0 + 4 * half - q.place);
+        const bool before = k0 + KT <= wave_place;
+        if (even_slopes && (before || k0 >= wave_place + 32)) {
+          const float slope = before ? q.slope : -q.slope, from = slope * (float)(4 * half);
+          bias0 = slope * (float)(k0 - q.place);
 #pragma unroll
-          for (int i = 0; i < KT / 2; ++i) bias[i] = fmaf(q.slope, (float)(at(i) - 4 * half), first);
+          for (int i = 0; i < KT / 2; ++i) bias[i] = fmaf(slope, (float)(at(i) - 4 * half), from);
         } else {
 #pragma unroll
           for (int i = 0; i < KT / 2; ++i) bias[i] = 0.0f;
@@ -596,23 +601,26 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
           add_place_bias<KT / 2>(q, s, key);
         }
         if (masked) hide<KT / 2>(q, s, key);
-        float top = m;
+        // (kPlace: the tile's scores and the maximum's both lack bias0)
+        float top = MODE == kPlace ? -INFINITY : m;
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) top = fmaxf(top, s[i]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) {
-          const float by = __builtin_amdgcn_exp2f((m - top) * a.exp_by);
+        float base = MODE == kPlace ? m - bias0 : m;
+        if (__any(top > base)) {
+          const float to = MODE != kPlace ? top : top > base ? top + bias0 : m, by = __builtin_amdgcn_exp2f((m - to) * a.exp_by);
           l *= by;
 #pragma unroll
           for (int t = 0; t < D / 32; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] *= by;
-          m = top;
+          m = to;
+          base = MODE == kPlace ? m - bias0 : m;
         }
-        float off = fmaf(m, a.exp_by, -kExpRaise<T, BITS8>);
+        float off = fmaf(base, a.exp_by, -kExpRaise<T, BITS8>);
         const bool large = fabsf(off) > kMostOffset;
         if (__any(large)) {  // (of this row: others keep their bits)
-          const float first = large ? m : 0.0f;
+          const float first = large ? base : 0.0f;
           off = large ? -kExpRaise<T, BITS8> : off;
 #pragma unroll
           for (int i = 0; i < KT / 2; ++i) s[i] -= first;

@@ -7,6 +7,7 @@ import torch
 
 from paper_2401_06145_amd import binding as B
 from tests import cache_ref as cref
+from tests import transformer_ref as ref
 from tests.cache_ref import Cached, check_attention
 from tests.gpu_helpers import DEV, say
 
@@ -92,3 +93,48 @@ def test_rows_do_not_go_by_others(bits8, dtype):
         got = b.run()
         got[1, 2] = clean[1, 2]
         assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("source", ["pages", "pages of 8 bits", "packed"])
+@pytest.mark.parametrize("slopes", [[-0.25, -0.25], [0.25, -0.25]])
+def test_far_keys_of_negative_slopes(slopes, source, dtype):
+    """Far keys with large biases: what their products add is small beside those, and must not be lost step by step.
+    Biases are multiples of 128 from 2^20 on in units of the products, where float32's step is 1/8; every second key has 96
+    products of 2^-8, together 3 steps, of which 16 are half of one.  Bias, product and sum are float32 numbers."""
+    say(f"slopes {slopes}, {source} {dtype}")
+    n, nq, d = 66_000, 150, 128
+    k = torch.zeros((n, 1, d), device=DEV)
+    k[::2, :, :96] = 2.0 ** -5
+    k[..., 127] = 448 * 2.0 ** -9  # (rows of 8 bits have a scale of 2^-9)
+    g = torch.Generator(DEV).manual_seed(18)
+    b = Cached([nq], [n], 2, 1, d, dtype, source == "pages of 8 bits", 32, seed=18,
+               like=(k, torch.randn((n, 1, d), device=DEV, generator=g)))
+    b.q[:] = 0.0
+    b.q[..., :96] = 2.0 ** -3
+    kw = dict(scale=2.0 ** -6, slopes=torch.tensor(slopes, device=DEV))
+    if source == "packed":
+        got = B.attention(b.q, b.k.to(dtype), b.v.to(dtype), b.q_start, cref.starts([n]), nq, n, causal=True, **kw)
+    else:
+        got = b.run(**kw)
+    check_attention(got, *b.want(**kw), source)
+
+
+def test_queries_before_the_first_key():
+    """More queries than keys: the first stand before all keys, and see a prefix of them from afar.
+
+    A score of a bias of up to 2 x 700 is rounded to float32 where the bias is added, by at most 1400 x 2^-24 (half a step
+    relative to its size), which is a factor of as much of its exponential: of each of a row's sum of values and
+    its sum of exponentials, so of their quotient twice that, 1.7e-4, beside what the bound counts anyway (products, and
+    distances of some hundred)."""
+    say("queries before the first key, with slopes")
+    for dtype in (F32, F16, BF16):
+        for bits8 in (False, True):
+            b = Cached([700, 150], [90, 300], 4, 2, D, dtype, bits8, 16, seed=19)
+            slopes = torch.tensor([0.5, -0.5, 0.01, 2.0], device=DEV)
+            for kw in (dict(prefix=[40, 5]), dict(causal=False)):
+                got, (want, mag) = b.run(slopes=slopes, **kw), b.want(slopes=slopes, **kw)
+                u = ref.UNIT[dtype]
+                bound = mag * (2 * u + 4e-5 + 2 * 1400 * 2.0 ** -24) + want.abs() * u + 2 * ref.TINY[dtype]
+                off = (got.double() - want).abs()
+                assert bool((off <= bound).all()), f"{kw} {dtype}: off by {float((off / bound).max()):.2f} of the bound"
