@@ -655,6 +655,8 @@ class Pages:
     def make(cls, pages: int, page: int, kv_heads: int, head_dim: int, dtype: torch.dtype, bits8: bool = False,
              device="cuda") -> "Pages":
         """Pages of zeros."""
+        if not 1 <= page <= 1 << 16 or page & (page - 1):
+            raise ValueError(f"rows of a page: expected a power of two up to 65536, got {page}")
         shape = (pages, kv_heads, page, head_dim)
         if not bits8:
             return cls(*(torch.zeros(shape, dtype=dtype, device=device) for _ in range(2)))

@@ -95,17 +95,28 @@ class PagedCaches:
             raise ValueError(f"a document of {max(lens)} tokens does not fit {self.table.shape[1]} pages of {self.page}")
         if sum(more) > len(self.free):
             raise ValueError(f"{sum(more)} more pages are needed, and {len(self.free)} are free")
-        at, of = [], []
+        at = []
         for t, m in enumerate(more):
-            for _ in range(m):
-                at.append(t * self.table.shape[1] + len(self.held[t]))
-                of.append(self.free.pop())
-                self.held[t].append(of[-1])
+            at.extend(t * self.table.shape[1] + len(self.held[t]) + i for i in range(m))
+        of = self.free[:-len(at) - 1:-1]  # from the end, as they are given out
         if at:
             both = torch.tensor([at, of], dtype=torch.int64).to(self.table.device)
             self.table.view(-1)[both[0]] = both[1].to(torch.int32)
-        self.lens = lens
         self.length += torch.tensor(new, dtype=torch.int32).to(self.length.device)
+        # the host's side last: what raised above has changed nothing that a call reads
+        del self.free[len(self.free) - len(at):]
+        for t, m in enumerate(more):
+            self.held[t].extend(of[:m])
+            del of[:m]
+        self.lens = lens
+
+    def shrink(self, new: list) -> None:
+        """Takes the last new[t] tokens of each document t back, as if they had not come."""
+        self.length -= torch.tensor(new, dtype=torch.int32).to(self.length.device)
+        self.lens = [a - b for a, b in zip(self.lens, new)]
+        for held, n in reversed(list(zip(self.held, self.lens))):
+            while len(held) > -(-n // self.page):
+                self.free.append(held.pop())
 
     def release(self, doc: int) -> None:
         """Document ``doc`` ends: its pages are free, and its place is an empty document's."""
@@ -246,11 +257,23 @@ class Transformer:
 
     def extend(self, x: torch.Tensor, new: list, caches: PagedCaches) -> torch.Tensor:
         """New tokens for each document, any number (a prompt, its next chunk, one token, none): rows
-        x [sum(new)][width] in the documents' order; the caches grow by them."""
+        x [sum(new)][width] in the documents' order; the caches grow by them, or, where the call raises, stay as
+        they were.  Tokens see of their document's prefix what has come with this call: a prefix that all of
+        it should see comes in one.  Heads turn by place (voxels are ``forward``'s)."""
         if len(x) != sum(new):
             raise ValueError(f"{sum(new)} new tokens, but {len(x)} rows")
+        if len(x) and (x.dim() != 2 or x.shape[1] != self.config.width or x.dtype != self.dtype or x.device != caches.table.device):
+            raise ValueError(f"x: expected {self.dtype} rows of {self.config.width} on {caches.table.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
         first = caches.length.clone()
         caches.grow(new)
+        try:
+            return self._extend(x, new, caches, first) if len(x) else x
+        except BaseException:
+            caches.shrink(new)
+            raise
+
+    def _extend(self, x: torch.Tensor, new: list, caches: PagedCaches, first: torch.Tensor) -> torch.Tensor:
         start = torch.tensor([sum(new[:t]) for t in range(len(new) + 1)], dtype=torch.int32).to(self.device)
 
         def attend(i, q, k, v):
@@ -258,7 +281,7 @@ class Transformer:
             return B.cached_attention(q, caches.layers[i], start, caches.length, caches.table, max(new), max(caches.lens),
                                       prefix=caches.prefix, cap=self.config.cap)
 
-        return self._run(x, attend, self._places(len(x), start, first)) if len(x) else x
+        return self._run(x, attend, self._places(len(x), start, first))
 
 
 def main() -> None:
