@@ -436,7 +436,8 @@ typedef struct {
  * it goes to place k_len[t] - (q_start[t + 1] - q_start[t]) + i.  Rows of no document, and places
  * before 0 or behind the table, are left out.  d_k, d_v: rows n, kv_heads, head_dim in `dtype`, 16-byte
  * aligned, strides multiples of 16 bytes.  Two rows for one place (documents that share a page)
- * leave either's elements.  Rows up to what one launch takes (2^32 threads, 256 for at most 64 rows:
+ * leave either's elements, in 8 bits with either's scale: equal rows are safe, others are the caller's
+ * to keep apart.  Rows up to what one launch takes (2^32 threads, 256 for at most 64 rows:
  * SPCONV_EUNSUPPORTED beyond), here and in spconv_cache_read. */
 int spconv_cache_write(const spconv_pages* pages, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
                        int64_t v_row, int64_t v_head, const int32_t* d_q_start, const int32_t* d_k_len, int64_t n,
@@ -450,8 +451,8 @@ int spconv_cache_read(const spconv_pages* pages, void* d_k, int64_t k_row, int64
 
 /* spconv_attention over pages: document t's keys are its k_len[t] (at most table_row * page) in
  * the pages, its queries the new tokens (one, or a chunk), whose keys are among them.  Of `args`
- * d_k, d_v, their strides, d_k_start and n_k are not used, d_k_len has to be given, and voxels are
- * not supported; n_docs, kv_heads and head_dim are those of the pages.  The rest is as there: its
+ * d_k, d_v, their strides, d_k_start and n_k are not used (n_k has to be a number that
+ * spconv_attention takes, as 0 is), d_k_len has to be given, and voxels are not supported; n_docs, kv_heads and head_dim are those of the pages.  The rest is as there: its
  * masks, prefix, cap, bias by place, rows that stay as they are, and limits.  8-bit rows count as
  * the exact values that they stand for, except with float16 queries where those are beyond that
  * type's range or subnormal in it.  More than 2^31 - 1 rows of queries times heads of a key head:

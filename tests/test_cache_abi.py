@@ -215,3 +215,12 @@ def test_queries_of_a_key_head_have_31_bits():
     assert attend(pages(kv_heads=1), n_q=1 << 30, kv_heads=1, max_q=1 << 30) == B.SPCONV_EUNSUPPORTED
     assert B.spconv_cached_attention_workspace_bytes(pages(kv_heads=1), attention_args(n_q=1 << 30, kv_heads=1, max_q=1 << 30)) == 0
     assert write(pages(kv_heads=1 << 12, page=1 << 16, head_dim=64, table_row=1)) == B.SPCONV_EUNSUPPORTED
+
+
+def test_rows_of_packed_keys_are_no_part_of_cached_attention():
+    """n_k may be any number that the packed call takes; nothing goes by it."""
+    p = pages(table_row=2000)
+    need = [B.spconv_cached_attention_workspace_bytes(p, attention_args(n_q=1, max_q=1, max_k=20_000, d_k_len=P, n_k=n, d_k=None,
+                                                                        d_v=None, d_k_start=None, k_row=3, v_head=-1))
+            for n in (0, 9, 20_000, (1 << 31) - 1)]
+    assert need[0] > 0 and len(set(need)) == 1
