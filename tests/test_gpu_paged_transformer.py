@@ -121,3 +121,85 @@ def test_documents_come_and_go():
     assert model.extend(rows[:0], [0, 0], caches).shape == (0, 256)
     with pytest.raises(ValueError):
         model.extend(rows[:3], [1, 1], caches)
+
+
+def run_pieces(model, rows, caches, calls):
+    """Outputs of each document, its calls one after the other."""
+    out, done = [[] for _ in rows], [0] * len(rows)
+    for new in calls:
+        y = model.extend(torch.cat([r[d:d + m] for r, d, m in zip(rows, done, new)]), new, caches)
+        for t, m in enumerate(new):
+            out[t].append(y[sum(new[:t]):sum(new[:t + 1])])
+            done[t] += m
+    return torch.cat([torch.cat(o) for o in out])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bits8", [False, True])
+def test_chunks_without_rotation_or_norms(bits8, dtype):
+    """The base configuration: what pages and chunks alone may change."""
+    say(f"transformer over pages, 8 bits {bits8}, {dtype}")
+    g = torch.Generator(DEV).manual_seed(4)
+    lens = [120, 5, 300, 40]
+    model = tr.Transformer(tr.Config(), dtype, DEV)
+    rows = [torch.randn((n, 256), device=DEV, generator=g).to(dtype) for n in lens]
+    got = run_pieces(model, rows, model.pages(4, 40, page=16, bits8=bits8, most=20), pieces(lens))
+    want = model.forward(torch.cat(rows), starts(lens), max(lens), causal=True)
+    # 8-bit keys and values add the rounding of two more products
+    assert off(got, want) < ROUNDED / 2 * (1.5 if bits8 else 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("kw", CONFIGS)
+def test_a_prefix_that_comes_in_one_call(kw, bits8, dtype):
+    """Is seen by all of its document's tokens, as in whole documents."""
+    say(f"transformer over pages with {kw} and a prefix, 8 bits {bits8}, {dtype}")
+    g = torch.Generator(DEV).manual_seed(5)
+    lens, first = [120, 5, 300, 40], [64, 5, 100, 40]
+    prefix = torch.tensor([60, 0, 100, 33], dtype=torch.int32, device=DEV)
+    model = tr.Transformer(tr.Config(**kw), dtype, DEV)
+    rows = [torch.randn((n, 256), device=DEV, generator=g).to(dtype) for n in lens]
+    caches = model.pages(4, 40, page=16, bits8=bits8, most=20, prefix=prefix)
+    got = run_pieces(model, rows, caches, [first, [1, 0, 1, 0], [55, 0, 70, 0], [0, 0, 129, 0]])
+    want = model.forward(torch.cat(rows), starts(lens), max(lens), causal=True, prefix=prefix)
+    assert off(got, want) < ROUNDED / 2 * (1.5 if bits8 else 1)
+    # and it matters: without it the first document's rows of the prefix are others
+    other = model.forward(torch.cat(rows), starts(lens), max(lens), causal=True)
+    assert off(want[:60], other[:60]) > 4 * ROUNDED
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("kw", CONFIGS)
+def test_a_prefix_that_comes_in_chunks(kw, bits8):
+    """Each call's tokens see of it what is there: one layer, whose keys go by its rows alone."""
+    say(f"transformer over pages with {kw} and a prefix in chunks, 8 bits {bits8}")
+    g = torch.Generator(DEV).manual_seed(6)
+    n, dtype = 90, torch.bfloat16
+    model = tr.Transformer(tr.Config(layers=1, **kw), dtype, DEV)
+    x = torch.randn((n, 256), device=DEV, generator=g).to(dtype)
+    caches = model.pages(1, 6, page=16, bits8=bits8, prefix=torch.tensor([60], dtype=torch.int32, device=DEV))
+    at = 0
+    for m in (20, 30, 1, 39):
+        got = model.extend(x[at:at + m], [m], caches)
+        at += m
+        seen = torch.tensor([min(60, at)], dtype=torch.int32, device=DEV)
+        want = model.forward(x[:at], starts([at]), at, causal=True, prefix=seen)[at - m:]
+        assert off(got, want) < ROUNDED / 2 * (1.5 if bits8 else 1)
+
+
+def test_a_refused_call_can_be_made_again():
+    """Rows that the call does not take change nothing; the same tokens as they should be give what they would have given."""
+    say("extend refused, and made again")
+    g = torch.Generator(DEV).manual_seed(7)
+    model = tr.Transformer(tr.Config(rotary=32), torch.bfloat16, DEV)
+    x = torch.randn((80, 256), device=DEV, generator=g).to(torch.bfloat16)
+    a, b = (model.pages(2, 9, page=16) for _ in range(2))
+    for c in (a, b):
+        model.extend(x[:50], [30, 20], c)
+    for bad in (x[50:].float(), x[50:, :128], x[50:].clone().requires_grad_(), x[50:].cpu()):
+        with pytest.raises(ValueError):
+            model.extend(bad, [17, 13], a)
+        assert a.lens == [30, 20] and a.length.tolist() == [30, 20] and a.free == b.free and a.held == b.held
+    assert torch.equal(model.extend(x[50:], [17, 13], a), model.extend(x[50:], [17, 13], b))
+    assert torch.equal(a.table[:, :2], b.table[:, :2]) and a.free == b.free
