@@ -18,8 +18,8 @@ HEADS, KV = 4, 2
 QL, KL = [100, 70], [200, 170]  # of the first document's keys 100 .. 199 are seen by some queries and not by others
 
 
-def documents(d, dtype, bits8):
-    return Cached(QL, KL, HEADS, KV, d, dtype, bits8, 16, seed=d)
+def documents(d, dtype, bits8, ql=QL):
+    return Cached(ql, KL, HEADS, KV, d, dtype, bits8, 16, seed=d)
 
 
 def row_of(b, place):
@@ -33,8 +33,9 @@ def check(b, clean, place, head, columns, is_value):
     got = b.run()
     sees = torch.zeros(got.shape, dtype=torch.bool, device=DEV)
     group = HEADS // KV
-    first = QL[0] - (KL[0] - place)
-    sees[max(first, 0):QL[0], head * group:(head + 1) * group, columns] = True
+    queries = b.q_lens[0]
+    first = queries - (KL[0] - place)
+    sees[max(first, 0):queries, head * group:(head + 1) * group, columns] = True
     assert bool(is_value(got[sees]).all()), f"key {place}: a query that sees it has not got its value"
     other = got[~sees]
     assert torch.equal(other, clean[~sees]), (f"key {place}: {int((other != clean[~sees]).sum())} values of "
@@ -125,3 +126,21 @@ def test_packed_keys():
             w[place, 1, d - 1] = math.nan
             b.run = lambda: run(w)
             check(b, clean, place, 1, d - 1, torch.isnan)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("d", [16, 48, 80, 96, 128, 256])
+def test_few_queries(d, bits8, dtype):
+    """Five new tokens: each sees its own place and those before."""
+    b = documents(d, dtype, bits8, ql=[5, 1])
+    clean = b.run()
+    v = b.cache.v.view(torch.uint8) if bits8 else b.cache.v
+    for place in range(190, 200):
+        for column in (0, d // 2 + 3, d - 1):
+            say(f"few queries, 8 bits {bits8}, {d} columns {dtype}: NaN at key {place}, column {column}")
+            page, row = row_of(b, place)
+            kept = v[page, 1, row, column].clone()
+            v[page, 1, row, column] = 0x7f if bits8 else math.nan
+            check(b, clean, place, 1, column, torch.isnan)
+            v[page, 1, row, column] = kept
