@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   f32x4 v = {0, 0, 0, 0};
   for (int s0 = 0; s0 < a.splits; s0 += kWave) {
     const int s = s0 + lane;
-    float by = 0.0f;
+    float by = -1.0f;  // less than any weight: nothing to add (a weight of 0 still makes NaN of a NaN)
     if (s < a.splits) {
       const f32x2 ml = a.part_ml[(int64_t)s * rows + at];
       if (ml[1] != 0.0f) {  // a range without keys has written nothing else
@@ -107,9 +107,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
       for (int u = 0; u < 4; ++u) {
         const int i = i0 + u * groups + lane / wide;
         const float from = __shfl(by, i);
-        w[u] = i < here ? from : 0.0f;
+        w[u] = i < here ? from : -1.0f;
         p[u] = f32x4{0, 0, 0, 0};
-        if (w[u] != 0.0f && x < a.d)
+        if (w[u] >= 0.0f && x < a.d)
           p[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + i) * rows + at) * a.d + x);
       }
 #pragma unroll

@@ -144,3 +144,31 @@ def test_few_queries(d, bits8, dtype):
             v[page, 1, row, column] = 0x7f if bits8 else math.nan
             check(b, clean, place, 1, column, torch.isnan)
             v[page, 1, row, column] = kept
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n", [2000, 5000, 40_000])
+def test_a_nan_of_no_weight(n, dtype):
+    """A value that is seen with a weight below float32's least number: 0 times NaN is NaN, however many ranges of keys
+    a row is joined from (1 to 8, more, and more than a wave has lanes)."""
+    say(f"one token of {n} keys {dtype}: a NaN of no weight")
+    d = 64
+    k = torch.zeros((n, 1, d), device=DEV)
+    k[:n // 3, :, 0] = -300.0  # whole ranges
+    b = Cached([1], [n], 2, 1, d, dtype, False, 16, seed=n % 97, like=(k, torch.randn((n, 1, d), device=DEV)))
+    b.q[:] = 0.0
+    b.q[..., 0] = 1.0
+    start = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    packed_k, packed_v = b.k.to(dtype), b.v.to(dtype)
+
+    def both():
+        return (b.run(scale=1.0), B.attention(b.q, packed_k, packed_v, b.q_start, start, 1, n, causal=True, scale=1.0))
+
+    clean = both()
+    page, row = row_of(b, 3)
+    b.cache.v[page, 0, row, 5] = math.nan
+    packed_v[3, 0, 5] = math.nan
+    for got, was, what in zip(both(), clean, ("pages", "packed keys")):
+        assert bool(got[..., 5].isnan().all()), what
+        got[..., 5] = was[..., 5]
+        assert torch.equal(got, was), what
