@@ -11,7 +11,10 @@
 // only, and its exponentials are, as they lie, the second operand of out^T = V^T P^T.
 // P is rounded to the rows' type for that product, which is what the matrix unit multiplies at full
 // rate; sums of P are not.  The rounding is at most that of the result once more (bfloat16: 0.0019
-// to 0.0023 of the result in place of 0.0017, float16 and float32 even).
+// to 0.0023 of the result in place of 0.0014 to 0.0017, float16 0.00024 in place of 0.00021, from 8-bit pages 0.00032 in
+// place of 0.00022; float32 even).  What it leaves off as a second operand, twice the products with V, would give that
+// back, and takes: chunks of 1024 over pages 577 -> 739 us, over 8-bit pages 681 -> 905, 512 of float16 113 -> 141,
+// single tokens 157 -> 158 and 103 -> 106.
 #include "attention_device.h"
 
 namespace spc {

@@ -25,7 +25,8 @@ constexpr int most_columns(int row) { return row <= 128 ? 64 : row <= 256 ? 32 :
 // the lanes that load that key's row.  8-bit rows: K comes 16 columns a lane (the product's columns
 // may be in any order, as long as the queries' are in the same), V widened into the strip.  Bound by
 // memory as packed keys are, 8 bits by the loads under way: one token for each of 48 documents of up to 8192
-// keys, 32 heads of 128 on 8, 1.20 GB: 229 us (5.2 TB/s); in 8 bits, 0.62 GB, 143 us (4.3 TB/s, the join included).
+// keys, 32 heads of 128 on 8, 1.20 GB: 230 us (5.2 TB/s); in 8 bits, 0.62 GB, 144 us (4.3 TB/s, the join included); in float32,
+// 2.40 GB, 520 us (4.6 TB/s; packed keys 435).
 template <typename T, int D, int NC, int SRC>
 __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   typedef typename Mat<T>::Frag Frag;
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(256, NC == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     } else if (!AHEAD) {
       fetch_pages(k0 + 4 * KT);
     }
-    Frag fp[NC];
+    Frag fp[NC];  // rounded to the rows' type (attention.hip has why, and what it costs in the result)
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
       float sc[8];

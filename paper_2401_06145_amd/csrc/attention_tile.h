@@ -118,11 +118,12 @@ struct Near {
 // Pages: a tile's rows are the queries of all heads of a key head, next to each other.  A wave's load covers rows_of_load rows.  Pages of that many rows or more (a power of two, as all
 // are) hold them together: the page's number is looked up a tile ahead and the rows' address is the
 // wave's, by scalar instructions.  Smaller ones (kSmall): each lane looks up the page of its row and
-// computes its address (4 x 1024 queries of 16,384 keys, 32 heads of 128: 1540 us so for pages of 64).
+// computes its address (4 x 1024 queries of 16,384 keys, 32 heads of 128: pages of 64 to 4 rows 1169 to 1226 us, of
+// 2 and 1, which go so, 1605 and 1712; in 8 bits of 64 and 8 1392 and 1407, of 4 to 1 1606 to 1701).
 // 8 bits: rows come into registers, and are widened into the other half of LDS when the tile is
-// done, once for all waves.  4 x 1024 queries of up to 16,384 keys, 32 heads of 128 on 8, bfloat16: packed keys
-// 1085 us, pages 1134 (0.94 PFLOP/s), 8 bits 1360 (0.78): two products a score, its scales from LDS and the
-// widening are 60 % more vector instructions, and the waves wait for LDS.
+// done, once for all waves.  4 x 1024 queries of 16,384 keys, 32 heads of 128 on 8, bfloat16: packed keys
+// 1085 to 1134 us, pages 1134 to 1177 (0.94 PFLOP/s), 8 bits 1360 to 1400 (0.78): two products a score, its scales from
+// LDS and the widening are 53 % more vector instructions, and the waves wait for LDS.  Capped at 30: 1354, 1435, 1635.
 constexpr int rows_of_load(int d, int e, bool bits8) {
   const int chunks = lds_columns(d) * (bits8 ? 1 : e) / 16;  // of a row
   return chunks >= kWave ? 1 : kWave / chunks;
@@ -638,7 +639,7 @@ __global__ __launch_bounds__(256, waves_a_simd(lds_columns(D) * sizeof(T), MODE,
 #pragma unroll
         for (int i = 0; i < KT / 2; ++i) s[i] *= sscale[b][1][8 * (i / 16) + 2 * (i % 16 / 4) + half][i % 4];
       }
-      Frag fp[KT / 16];
+      Frag fp[KT / 16];  // rounded to the rows' type (attention.hip has why, and what it costs in the result)
 #pragma unroll
       for (int c = 0; c < KT / 16; ++c) fp[c] = to_frag<T>(s + 8 * c);
       // all exponentials before the products: 712 -> 702 us where nothing else stands between them

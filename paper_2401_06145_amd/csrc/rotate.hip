@@ -9,7 +9,8 @@
 // read once and nothing is exchanged but the sum of squares.  Angles are products of float64,
 // of which whole turns are taken off before they become float32: at place 10^6 a float32 angle would
 // be off by 0.06.  What bounds it is memory: 65,536 rows of 40 heads of 128 in bfloat16, 1.34 GB,
-// 266 us (5.0 TB/s, what a large copy reaches); for one row the host's call (5.4 us, the kernel 2.5).
+// 266 us (5.0 TB/s, what a large copy reaches; float32 as well, 20,000 rows 167 us, but 411 with pairs side by side,
+// whose stores of eight columns fill half lines each); for one row the host's call (5.4 us, the kernel 3.5 under the profiler).
 #include <algorithm>
 #include <type_traits>
 
@@ -211,8 +212,9 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a, int g) {
 // Heads whose pairs or addresses fit no wide access (an odd width, an odd number of pairs): rows of
 // heads that follow each other come through LDS in 16-byte pieces, and go back so; a lane has single pairs of
 // a head, as above with W = 1.  From 2^23 elements on (41,323 rows of 20 heads of 33, 32 turned, bfloat16: element by
-// element from memory 175 us, 109 so; 6724 rows of 24 heads of 256, 50 turned, float16 110 and 90; but 2539
-// rows of 24 heads of 33 11.1 and 12.3).  Bound by the vector unit and LDS, a few instructions an element.
+// element from memory 151 us, 109 so).  Six widths and types, 20 to 256 columns, of 8 to 24 heads, staged against not:
+// 2^21 elements 0.99 to 1.84, 2^22 0.83 to 1.31, 2^23 0.74 to 1.13, 2^24 0.70 to 1.15, 2^25 0.67 to 1.01.  (The slow ends
+// are 100 of 128 columns turned and 7 heads of 33 with pairs side by side.)  Bound by the vector unit and LDS, a few instructions an element.
 constexpr int kStage = 4096;  // elements
 template <typename T, int I, bool INTER>
 __global__ __launch_bounds__(kThreads) void k_rotate_staged(RotateArgs a, int g, int tile_rows) {
